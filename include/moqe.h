@@ -328,6 +328,74 @@ MOQE_API moqe_status moqe_routed_qgemm_sorted_residual(const void* X_bf16, const
 MOQE_API moqe_status moqe_routed_qgemm_workspace_clear(void* workspace, size_t workspace_bytes, int M, int N, int K,
                                                        int E, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Floating-point experts: the same routed linear layer with experts in microscaled 4-bit floating point or unquantized
+ * (Section 3.1: the experts are variants of one full-precision model; here the cheapest and the dearest of them).  The
+ * paper names no floating-point format; these are the OCP Microscaling MXFP4, NVFP4 and plain bf16.
+ *   e2m1   : 0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign bit (codes 0..7, + 8 for the sign).  Rounding is to the nearest number of the
+ *            exact quotient, ties to the even code, beyond 6 to 6; the sign bit is that of the number.
+ *   MXFP4  : 32 consecutive k share a scale 2^e, stored as e + 127 (E8M0): e = max(floor(log2 max|x|) - 2, -127), -127 for zeros;
+ *            code = e2m1(x / 2^e).
+ *   NVFP4  : a row (a token, an output channel) has an fp32 scale o, 16 consecutive k an e4m3 scale s.  Rows quantized here take
+ *            o = 2^max(floor(log2 A) - 10, -126) with A the row's largest finite magnitude (1 for zeros), which leaves the products
+ *            exact; s = e4m3(max|x| / (6 o)), ties to even; code = e2m1(x / (s o)), magnitude 0 where s = 0.
+ *   Both   : the last block of a row may be short.  A block with an infinity or a NaN has the scale NaN (E8M0 255, e4m3 127)
+ *            and codes 0; the other blocks of its row are as without it.
+ * Canonical arrays: codes [rows][K / 2], two a byte, the even k in the low half; scales [rows][ceil(K / 32 or 16)], one byte each;
+ * outer fp32 [rows] (NVFP4 only); values bf16 [rows][K] = code * scale * outer, rounded once.  K % 8 == 0.
+ * ------------------------------------------------------------------------- */
+typedef enum { MOQE_FP_MXFP4 = 1, MOQE_FP_NVFP4 = 2, MOQE_FP_BF16 = 3 } moqe_fp_format;
+
+/* Rows of activations in a 4-bit format: exactly what a row's product with an expert of that format sees.  X bf16 [M][K],
+ * 16-byte aligned.  codes (16-byte aligned), scales, outer and values_bf16 (16-byte aligned) are written; any of them may be
+ * NULL, and outer is not written for MXFP4. */
+MOQE_API moqe_status moqe_fp4_quantize_rows(const void* X_bf16, int M, int K, int format, uint8_t* codes, uint8_t* scales,
+                                            float* outer, void* values_bf16, void* stream);
+
+/* One floating-point expert of one linear layer, on the device in the library's private packed layout. */
+typedef struct moqe_fp_expert moqe_fp_expert;
+
+/* Builds one from fp32 weights [N][K] (16-byte aligned) on `stream`; BF16 rounds to nearest even.  Memory as for
+ * moqe_quantize_rtn (pool, captures).  On success *out must be released with moqe_fp_expert_destroy. */
+MOQE_API moqe_status moqe_fp_quantize(const float* W, int N, int K, int format, void* stream, moqe_fp_expert** out);
+
+/* From canonical device arrays: codes (4-byte aligned), scales and outer for the 4-bit formats, values_bf16 [N][K] (16-byte
+ * aligned) for BF16; the others are not looked at.  outer NULL: 1.  An NVFP4 expert takes any fp32 outer (a checkpoint's tensor
+ * scale, repeated); the top bit of its scales is ignored. */
+MOQE_API moqe_status moqe_fp_expert_import(int N, int K, int format, const uint8_t* codes, const uint8_t* scales, const float* outer,
+                                           const void* values_bf16, void* stream, moqe_fp_expert** out);
+
+/* To canonical device arrays; any may be NULL, and those that the format does not have must be (BF16 has values only, MXFP4 no
+ * outer; MOQE_ERR_UNSUPPORTED).  values are rounded to bf16 once, which changes them only under an imported outer and at
+ * the ends of bf16's range. */
+MOQE_API moqe_status moqe_fp_expert_export(const moqe_fp_expert* e, uint8_t* codes, uint8_t* scales, float* outer, void* values_bf16,
+                                           void* stream);
+
+/* code_bytes = N*K/2 (BF16: 2*N*K); meta_bytes = scales and outer; alloc_bytes with the padding of channels to 128 and of k
+ * to 256 (BF16: 64).  Any output may be NULL. */
+MOQE_API moqe_status moqe_fp_expert_info(const moqe_fp_expert* e, int* N, int* K, int* format, size_t* code_bytes, size_t* meta_bytes,
+                                         size_t* alloc_bytes);
+/* Gives the expert's memory back, as moqe_expert_destroy does. */
+MOQE_API moqe_status moqe_fp_expert_destroy(moqe_fp_expert* e);
+
+/* The routed product, grouped by expert with ragged sizes, from one row to whole prompts:
+ *   Y[m][n] = bf16( sum_k xq[m][k] * w_e[n][k] ),   e = row_ids[m]
+ * with fp32 sums.  xq = the row quantized to the format of ITS expert (the values of moqe_fp4_quantize_rows) where that is a 4-bit
+ * format -- both operands have 4 bits and go to the tensor cores with their scales -- and the row itself where it is BF16.
+ * The experts of a call may have any mixture of formats; they agree on N (a multiple of 8) and K.  The same call gives the
+ * same bits.  workspace: moqe_routed_fpgemm_workspace(M, h_experts, E) bytes (0 for refused arguments), 256-byte aligned, contents
+ * irrelevant; the figure grows with M; calls that share a workspace must not overlap on the device.
+ * _sorted: `perm` [M] and `offsets` [E+1] as moqe_permute wrote them, not decreasing, within [0, M].  offsets[0] need not be 0: rows
+ * perm[0..offsets[0]) and perm[offsets[E]..M) of Y are left untouched, so that a batch over integer and floating-point
+ * experts takes one sort, moqe_routed_qgemm_sorted with the first offsets and this call with the rest.
+ * The unsorted call writes every row; those with an id outside [0,E) are zeros (MOQE_ERR_EXPERT_ID is latched). */
+MOQE_API size_t moqe_routed_fpgemm_workspace(int M, const moqe_fp_expert* const* h_experts, int E);
+MOQE_API moqe_status moqe_routed_fpgemm(const void* X_bf16, const int32_t* row_ids, int M, const moqe_fp_expert* const* h_experts, int E,
+                                        void* Y_bf16, void* workspace, size_t workspace_bytes, void* stream);
+MOQE_API moqe_status moqe_routed_fpgemm_sorted(const void* X_bf16, const int32_t* perm, const int32_t* offsets, int M,
+                                               const moqe_fp_expert* const* h_experts, int E, void* Y_bf16, void* workspace,
+                                               size_t workspace_bytes, void* stream);
+
 /* Synchronises `stream`, then returns and clears the first error latched by a
  * kernel on the current device (MOQE_OK if none). */
 MOQE_API moqe_status moqe_async_status(void* stream);

@@ -21,6 +21,7 @@ LIB_PATH = os.path.join(_HERE, "libmoqe.so")
 OK = 0
 ERR_NULL, ERR_SHAPE, ERR_UNSUPPORTED, ERR_ALLOC, ERR_WORKSPACE, ERR_MISMATCH, ERR_CUDA, ERR_EXPERT_ID, ERR_TIMEOUT, ERR_IO = range(1, 11)
 MAX_EXPERTS = 32
+FP_MXFP4, FP_NVFP4, FP_BF16 = 1, 2, 3
 PATH_AUTO, PATH_STREAM, PATH_TCGEN05, PATH_DECODE, PATH_DENSE = 0, 1, 2, 5, 6
 
 EXPORTED = (
@@ -33,6 +34,8 @@ EXPORTED = (
     "moqe_routed_qgemm_sorted_gated", "moqe_routed_qgemm_sorted_residual",
     "moqe_expert_offload", "moqe_expert_prefetch", "moqe_expert_host_info", "moqe_expert_host_save", "moqe_expert_host_load",
     "moqe_expert_host_destroy",
+    "moqe_fp4_quantize_rows", "moqe_fp_quantize", "moqe_fp_expert_import", "moqe_fp_expert_export", "moqe_fp_expert_info",
+    "moqe_fp_expert_destroy", "moqe_routed_fpgemm_workspace", "moqe_routed_fpgemm", "moqe_routed_fpgemm_sorted",
 )
 
 
@@ -95,6 +98,16 @@ def lib() -> C.CDLL:
         L.moqe_router_mlp_workspace.restype = sz
         L.moqe_router_mlp.argtypes = [vp, vp, i32, i32, vp, i32, vp, i32, vp, vp, vp, sz, vp]
         L.moqe_router_load_report.argtypes = [vp, vp, i32, i32, vp, vp, vp]
+        L.moqe_fp4_quantize_rows.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, vp]
+        L.moqe_fp_quantize.argtypes = [vp, i32, i32, i32, vp, C.POINTER(vp)]
+        L.moqe_fp_expert_import.argtypes = [i32, i32, i32, vp, vp, vp, vp, vp, C.POINTER(vp)]
+        L.moqe_fp_expert_export.argtypes = [vp, vp, vp, vp, vp, vp]
+        L.moqe_fp_expert_info.argtypes = [vp] + [C.POINTER(i32)] * 3 + [C.POINTER(sz)] * 3
+        L.moqe_fp_expert_destroy.argtypes = [vp]
+        L.moqe_routed_fpgemm_workspace.argtypes = [i32, vp, i32]
+        L.moqe_routed_fpgemm_workspace.restype = sz
+        L.moqe_routed_fpgemm.argtypes = [vp, vp, i32, vp, i32, vp, vp, sz, vp]
+        L.moqe_routed_fpgemm_sorted.argtypes = [vp, vp, vp, i32, vp, i32, vp, vp, sz, vp]
         L.moqe_launch_count.argtypes = []
         L.moqe_launch_count.restype = C.c_ulonglong
         _lib = L
@@ -440,6 +453,127 @@ def moqe_routed_qgemm_sorted_multi(Xs: Sequence[torch.Tensor], perm: torch.Tenso
     _check(lib().moqe_routed_qgemm_sorted_multi(_at(xa), _ptr(perm), _ptr(offsets), M, nl, _at(ea), E, _at(ya), _ptr(workspace),
                                                 workspace.numel(), _stream()), "moqe_routed_qgemm_sorted_multi")
     return Ys
+
+
+class FpExpert:
+    """Owner of one ``moqe_fp_expert*`` (destroyed with the Python object)."""
+
+    def __init__(self, handle: int):
+        self.handle = C.c_void_p(handle)
+        N, K, fmt = (C.c_int() for _ in range(3))
+        cb, mb, ab = (C.c_size_t() for _ in range(3))
+        _check(lib().moqe_fp_expert_info(self.handle, N, K, fmt, cb, mb, ab), "moqe_fp_expert_info")
+        self.N, self.K, self.format = N.value, K.value, fmt.value
+        self.code_bytes, self.meta_bytes, self.alloc_bytes = cb.value, mb.value, ab.value
+
+    @property
+    def address(self) -> int:
+        return (self.handle.value or 0) if self.handle is not None else 0
+
+    def close(self):
+        if self.handle is not None and self.handle.value:
+            lib().moqe_fp_expert_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def _fp_blocks(K: int, fmt: int) -> int:
+    return -(-K // (32 if fmt == FP_MXFP4 else 16))
+
+
+def moqe_fp4_quantize_rows(X: torch.Tensor, fmt: int, values: bool = False):
+    """Rows of bf16 ``X[M][K]`` in a 4-bit format: (codes uint8 ``[M][K/2]``, scales uint8 ``[M][blocks]``, outer fp32 ``[M]`` or
+    None, values bf16 ``[M][K]`` or None)."""
+    X = _dev(X, torch.bfloat16, "X")
+    M, K = X.shape
+    dev = X.device
+    codes = torch.empty((M, K // 2), dtype=torch.uint8, device=dev)
+    scales = torch.empty((M, _fp_blocks(K, fmt)), dtype=torch.uint8, device=dev)
+    outer = torch.empty(M, dtype=torch.float32, device=dev) if fmt == FP_NVFP4 else None
+    vals = torch.empty_like(X) if values else None
+    _check(lib().moqe_fp4_quantize_rows(_ptr(X), M, K, int(fmt), _ptr(codes), _ptr(scales), _ptr(outer), _ptr(vals), _stream()),
+           "moqe_fp4_quantize_rows")
+    return codes, scales, outer, vals
+
+
+def moqe_fp_quantize(W: torch.Tensor, fmt: int) -> FpExpert:
+    """The fp32 device matrix ``W[N][K]`` as an expert in ``FP_MXFP4``, ``FP_NVFP4`` or ``FP_BF16``."""
+    W = _dev(W, torch.float32, "W")
+    N, K = W.shape
+    out = C.c_void_p()
+    _check(lib().moqe_fp_quantize(_ptr(W), N, K, int(fmt), _stream(), C.byref(out)), "moqe_fp_quantize")
+    return FpExpert(out.value)
+
+
+def moqe_fp_expert_import(fmt: int, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
+                          outer: Optional[torch.Tensor] = None, values: Optional[torch.Tensor] = None) -> FpExpert:
+    """An expert from canonical arrays: ``codes``, ``scales`` and (NVFP4) ``outer``, or bf16 ``values[N][K]`` for ``FP_BF16``."""
+    if fmt == FP_BF16:
+        if values is None:
+            raise MoqeError(ERR_NULL, "moqe_fp_expert_import")
+        values = _dev(values, torch.bfloat16, "values")
+        (N, K), codes, scales, outer = values.shape, None, None, None
+    else:
+        if codes is None or scales is None:
+            raise MoqeError(ERR_NULL, "moqe_fp_expert_import")
+        codes, scales, values = _dev(codes, torch.uint8, "codes"), _dev(scales, torch.uint8, "scales"), None
+        outer = None if outer is None or fmt == FP_MXFP4 else _dev(outer, torch.float32, "outer")
+        N, K = codes.shape[0], 2 * codes.shape[1]
+        if tuple(scales.shape) != (N, _fp_blocks(K, fmt)) or (outer is not None and outer.numel() != N):
+            raise MoqeError(ERR_SHAPE, "moqe_fp_expert_import")
+    out = C.c_void_p()
+    _check(lib().moqe_fp_expert_import(N, K, int(fmt), _ptr(codes), _ptr(scales), _ptr(outer), _ptr(values), _stream(), C.byref(out)),
+           "moqe_fp_expert_import")
+    return FpExpert(out.value)
+
+
+def moqe_fp_expert_export(e: FpExpert, values: bool = False):
+    """-> (codes, scales, outer, values) as ``moqe_fp4_quantize_rows`` gives them; only values for an ``FP_BF16`` expert."""
+    dev = torch.device("cuda", torch.cuda.current_device())
+    four = e.format != FP_BF16
+    codes = torch.empty((e.N, e.K // 2), dtype=torch.uint8, device=dev) if four else None
+    scales = torch.empty((e.N, _fp_blocks(e.K, e.format)), dtype=torch.uint8, device=dev) if four else None
+    outer = torch.empty(e.N, dtype=torch.float32, device=dev) if e.format == FP_NVFP4 else None
+    vals = torch.empty((e.N, e.K), dtype=torch.bfloat16, device=dev) if values or not four else None
+    _check(lib().moqe_fp_expert_export(e.handle, _ptr(codes), _ptr(scales), _ptr(outer), _ptr(vals), _stream()), "moqe_fp_expert_export")
+    return codes, scales, outer, vals
+
+
+def moqe_routed_fpgemm_workspace(M: int, experts: Sequence[FpExpert]) -> int:
+    arr = _handles(experts)
+    return int(lib().moqe_routed_fpgemm_workspace(int(M), arr.buffer_info()[0], len(experts)))
+
+
+def moqe_routed_fpgemm(X: torch.Tensor, row_ids: torch.Tensor, experts: Sequence[FpExpert], Y: Optional[torch.Tensor] = None,
+                       workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """``Y[m] = xq[m] . W_{row_ids[m]}^T``: the routed product of floating-point experts of any mixture of formats."""
+    X = _dev(X, torch.bfloat16, "X")
+    row_ids = _dev(row_ids, torch.int32, "row_ids")
+    M, E = X.shape[0], len(experts)
+    if E == 0 or row_ids.numel() != M or X.shape[1] != experts[0].K:
+        raise MoqeError(ERR_SHAPE, "moqe_routed_fpgemm")
+    if Y is None:
+        Y = torch.empty((M, experts[0].N), dtype=torch.bfloat16, device=X.device)
+    if workspace is None:
+        workspace = alloc_workspace(moqe_routed_fpgemm_workspace(M, experts), X.device)
+    arr = _handles(experts)
+    _check(lib().moqe_routed_fpgemm(_ptr(X), _ptr(row_ids), M, arr.buffer_info()[0], E, _ptr(Y), _ptr(workspace), workspace.numel(),
+                                    _stream()), "moqe_routed_fpgemm")
+    return Y
+
+
+def moqe_routed_fpgemm_sorted(X: torch.Tensor, perm: torch.Tensor, offsets: torch.Tensor, experts: Sequence[FpExpert],
+                              Y: torch.Tensor, workspace: torch.Tensor, _arr=None) -> torch.Tensor:
+    """The same for a batch that ``moqe_permute`` has sorted; rows before ``offsets[0]`` and behind ``offsets[E]`` keep their ``Y``."""
+    arr = _arr if _arr is not None else _handles(experts)
+    _check(lib().moqe_routed_fpgemm_sorted(_ptr(X), _ptr(perm), _ptr(offsets), X.shape[0], _at(arr), len(experts), _ptr(Y),
+                                           _ptr(workspace), workspace.numel(), _stream()), "moqe_routed_fpgemm_sorted")
+    return Y
 
 
 def moqe_async_status() -> int:

@@ -1,0 +1,200 @@
+// Floating-point experts: microscaled 4-bit formats (MXFP4, NVFP4) and plain bf16.
+//
+// A 4-bit number is e2m1 (0, .5, 1, 1.5, 2, 3, 4, 6 and a sign bit); 32 (MXFP4) or 16 (NVFP4) consecutive k share a scale, a
+// power of two (E8M0) or an e4m3 number; an NVFP4 row has an fp32 scale of its own on top.  See moqe.h for the arithmetic.
+//
+// Every rounding here is that of an exact real quotient.  MXFP4 divides by a power of two.  NVFP4 divides by an e4m3 number: for
+// a source of bf16 a quotient that is not half way between two numbers is at least 2^-9 of its size away from there, for fp32
+// 2^-24 of its size, so that the correctly rounded fp32 quotient can meet a half way mark it should not meet with fp32 sources
+// only, and there the sign of the remainder decides (nv_quotient).
+//
+// Packed layout, the same for experts and for a call's token rows: k-blocks of 128 bytes a row (256 codes or 64 bf16), in which a
+// row's eight 16-byte chunks are permuted by the 128-byte swizzle (chunk c of row r at place c ^ (r & 7)), eight rows to 1024
+// bytes: what the tensor cores read K-major, so that a bulk copy without a tensor map brings an operand tile.  Scales stand in
+// the order that tensor memory wants, 512 bytes for 128 rows x 4 scales: row r, scale j at (r % 32) * 16 + (r / 32) * 4 + j.
+//   expert : tile (nt, kb) = 128 channels: 16 KB codes, then their scales (MXFP4 1 KB, NVFP4 2 KB); tiles ordered [nt][kb],
+//            one bulk copy each.  Then NVFP4's channel scales, fp32 [Np].  Rows and k behind the matrix are zeros.
+//   tokens : the rows of an expert start at a multiple of 128 rows (`pad0`); codes [kb][row / 8][1024 bytes], so that the
+//            rows of any tile are one piece; scales [row / 128][kb][1 or 2 KB]; row scales fp32.
+#pragma once
+#include "common.cuh"
+
+struct moqe_fp_expert {
+    int N, K, format;             // as given by the caller
+    int Np, KB;                   // channels padded to 128; k-blocks
+    int device;
+    bool pooled;
+    uint8_t* tiles;
+    float* outer;                 // NVFP4: [Np], behind the tiles
+    size_t tiles_alloc, outer_alloc;
+};
+
+namespace moqe {
+
+__host__ __device__ inline int fp_block(int format) { return format == MOQE_FP_MXFP4 ? 32 : 16; }       // k that share a scale
+__host__ __device__ inline int fp_kbk(int format) { return format == MOQE_FP_BF16 ? 64 : 256; }         // k of a k-block
+__host__ __device__ inline int fp_sf_bytes(int format) { return format == MOQE_FP_MXFP4 ? 1024 : format == MOQE_FP_NVFP4 ? 2048 : 0; }   // scales of 128 rows, a k-block
+__host__ __device__ inline int fp_tile_stride(int format) { return 16384 + fp_sf_bytes(format); }
+__host__ __device__ inline int fp_kblocks(int K, int format) { const int b = fp_kbk(format); return (K + b - 1) / b; }
+
+// Where one row of a packed matrix lies.
+struct PackedRow {
+    uint8_t* codes; size_t codes_kb;      // first k-block's 128 bytes of the row; from k-block to k-block
+    uint8_t* sf; size_t sf_kb;            // first scale of the row; from k-block to k-block
+    int r7;                               // row % 8
+    __device__ __forceinline__ uint8_t* chunk(int kb, int c) const { return codes + kb * codes_kb + ((c ^ r7) << 4); }
+    __device__ __forceinline__ uint8_t* scale(int kb, int b) const { return sf + kb * sf_kb + ((b >> 2) << 9) + (b & 3); }
+};
+__device__ __forceinline__ PackedRow expert_row(uint8_t* tiles, int KB, int format, int n) {
+    const int stride = fp_tile_stride(format), r = n & 127;
+    uint8_t* t = tiles + (size_t)(n >> 7) * KB * stride;
+    return {t + (r >> 3) * 1024 + (r & 7) * 128, (size_t)stride, t + 16384 + (r & 31) * 16 + (r >> 5) * 4, (size_t)stride, r & 7};
+}
+// row i of a segment of `pad` rows (a multiple of 128)
+__device__ __forceinline__ PackedRow token_row(uint8_t* codes, uint8_t* sf, int KB, int format, int i, int pad) {
+    const int sfb = fp_sf_bytes(format);
+    return {codes + (size_t)(i >> 3) * 1024 + (i & 7) * 128, (size_t)pad * 128,
+            sf + (size_t)(i >> 7) * KB * sfb + (i & 31) * 16 + ((i >> 5) & 3) * 4, (size_t)sfb, i & 7};
+}
+
+__device__ __forceinline__ float pow2_field(int field) { return __int_as_float(field << 23); }   // 2^(field - 127), 1 <= field <= 254
+__device__ __forceinline__ float e8m0_value(uint32_t b) { return b == 0 ? __int_as_float(0x00400000) : b == 255 ? __int_as_float(0x7FC00000) : pow2_field((int)b); }
+__device__ __forceinline__ float e4m3_value(uint32_t b) {       // 0 <= b <= 127
+    if (b == 127) return __int_as_float(0x7FC00000);
+    return b < 8 ? (float)b * 0x1p-9f : __int_as_float((int)((b << 20) + (120u << 23)));
+}
+
+// eight e2m1 codes, the first in the lowest nibble; to nearest, ties to the even code, beyond 6 to 6
+__device__ __forceinline__ uint32_t e2m1_x8(const float* v) {
+    uint32_t d;
+    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+        "mov.b32 %0, {a, b, c, d};\n\t}"
+        : "=r"(d) : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+    return d;
+}
+// what a code stands for
+__device__ __forceinline__ float e2m1_value(uint32_t c) {
+    const uint32_t m = c & 7u, sign = (c & 8u) << 28;
+    const uint32_t mag = m < 2 ? m * 0x3F000000u : ((m & 1u) << 22) + ((126u + (m >> 1)) << 23);
+    return __uint_as_float(mag | sign);
+}
+// nearest e4m3 number's byte, 0 <= v <= 448
+__device__ __forceinline__ uint32_t e4m3_byte(float v) {
+    uint16_t d;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(d) : "f"(0.f), "f"(v));
+    return d & 0xFFu;
+}
+
+// y / s for y >= 0 and an e4m3 number s > 0 with 1 / s correctly rounded in rs: the correctly rounded quotient (Markstein), moved
+// off a border by a unit of the last place where it is not there exactly (fp32 sources).
+template <bool FP32>
+__device__ __forceinline__ float nv_quotient(float y, float s, float rs) {
+    const float q0 = y * rs;
+    const float q = __fmaf_rn(__fmaf_rn(-q0, s, y), rs, q0);
+    if constexpr (FP32) {
+        const float rem = __fmaf_rn(-q, s, y);
+        const int bits = __float_as_int(q);
+        if ((bits & 0xFFFFF) == 0 && rem != 0.f) return __int_as_float(bits + (rem > 0.f ? 1 : -1));
+    }
+    return q;
+}
+
+// Scale and codes of 16 consecutive k of a row.  `amax`: bits of the largest magnitude of the numbers that share the scale;
+// `row_field`: NVFP4's row scale is 2^(row_field - 127).  -> the scale's byte; codes, eight to a word.
+template <int FORMAT, bool FP32>
+__device__ __forceinline__ uint32_t encode16(const float (&x)[16], uint32_t amax, int row_field, uint32_t (&codes)[2]) {
+    if (amax >= 0x7F800000u) {                              // an infinity or a NaN: the block is a NaN
+        codes[0] = codes[1] = 0;
+        return FORMAT == MOQE_FP_MXFP4 ? 255u : 127u;
+    }
+    float q[16];
+    uint32_t byte;
+    if constexpr (FORMAT == MOQE_FP_MXFP4) {
+        byte = (uint32_t)max((int)(amax >> 23) - 2, 0);
+        const float inv = pow2_field(254 - (int)byte);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) q[i] = x[i] * inv;
+    } else {
+        const float inv = pow2_field(254 - row_field);
+        byte = e4m3_byte(__fdiv_rn(__uint_as_float(amax) * inv, 6.0f));
+        const float s = e4m3_value(byte);
+        const float rs = byte ? __frcp_rn(s) : 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) q[i] = copysignf(nv_quotient<FP32>(fabsf(x[i]) * inv, s, rs), x[i]);
+    }
+    codes[0] = e2m1_x8(q);
+    codes[1] = e2m1_x8(q + 8);
+    return byte;
+}
+// NVFP4: the row scale's exponent field for the bits of the row's largest finite magnitude
+__device__ __forceinline__ int nv_row_field(uint32_t amax) { return amax == 0 ? 127 : max((int)(amax >> 23) - 10, 1); }
+
+// 16 consecutive k of a row, zeros behind its end (K is a multiple of 8)
+__device__ __forceinline__ void load16(const __nv_bfloat16* row, int k, int K, float (&x)[16]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint4 v = k + 8 * h < K ? *reinterpret_cast<const uint4*>(row + k + 8 * h) : make_uint4(0, 0, 0, 0);
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[8 * h + 2 * i] = __uint_as_float(w[i] << 16);
+            x[8 * h + 2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+        }
+    }
+}
+__device__ __forceinline__ void load16(const float* row, int k, int K, float (&x)[16]) {
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+        const float4 v = k + 4 * h < K ? *reinterpret_cast<const float4*>(row + k + 4 * h) : make_float4(0.f, 0.f, 0.f, 0.f);
+        x[4 * h] = v.x; x[4 * h + 1] = v.y; x[4 * h + 2] = v.z; x[4 * h + 3] = v.w;
+    }
+}
+__device__ __forceinline__ uint32_t magnitude_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+__device__ __forceinline__ uint32_t amax16(const float (&x)[16]) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) m = max(m, magnitude_bits(x[i]));
+    return m;
+}
+__device__ __forceinline__ uint32_t finite_amax16(const float (&x)[16]) {
+    uint32_t m = amax16(x);
+    if (m >= 0x7F800000u) {
+        m = 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) { const uint32_t b = magnitude_bits(x[i]); m = max(m, b < 0x7F800000u ? b : 0u); }
+    }
+    return m;
+}
+// the largest value of all threads of the block (a multiple of 32 threads); `buf`: 32 words
+__device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t* buf) {
+    v = __reduce_max_sync(0xFFFFFFFFu, v);
+    if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = threadIdx.x % 32 < blockDim.x / 32 ? buf[threadIdx.x & 31] : 0u;
+    return __reduce_max_sync(0xFFFFFFFFu, v);
+}
+
+// quantize.cu: device memory of experts (a pool of the library's)
+void* expert_malloc(size_t bytes, int device, cudaStream_t st, bool& pooled);
+bool expert_free(void* p, bool pooled, int device);
+
+// fp_rows.cu: the token rows of a sorted batch in their experts' formats
+struct FpTokens {
+    uint8_t *codes, *sf; float* outer;    // regions of the workspace
+    size_t row_bytes, block_sf;           // room for a row's codes, and for the scales of 128 rows: the largest of the call's formats
+};
+struct FpExperts { uint8_t format[MOQE_MAX_EXPERTS]; };
+moqe_status launch_fp_tokens(const void* X, const int32_t* perm, const int32_t* offsets, int M, int K, int E, const FpExperts& formats,
+                             const FpTokens& tokens, uint32_t* counters, int n_counters, cudaStream_t st);
+
+// fp_gemm.cu
+moqe_status launch_fp_gemm(const moqe_fp_expert* const* ex, int E, int M, const int32_t* perm, const int32_t* offsets, const FpTokens& tokens,
+                           uint32_t* counters, void* partials, void* Y, cudaStream_t st);
+int fp_gemm_counters();
+size_t fp_gemm_partial_bytes(int M);
+
+}  // namespace moqe

@@ -12,6 +12,7 @@
 #include <new>
 
 #include "dequant.cuh"
+#include "fp_formats.cuh"
 #include "ptx.cuh"
 
 namespace moqe {
@@ -640,6 +641,8 @@ cudaMemPool_t expert_pool(int device) {
     return g_pools[device];
 }
 
+}  // namespace
+
 // Memory for an expert that is filled on `st`, or nullptr.  A stream that is being captured gets memory from cudaMalloc, where the
 // capture's mode allows it: the pool's would belong to the graph.
 void* expert_malloc(size_t bytes, int device, cudaStream_t st, bool& pooled) {
@@ -658,7 +661,7 @@ void* expert_malloc(size_t bytes, int device, cudaStream_t st, bool& pooled) {
 // waits as it did when experts' own memory was given back with it: cudaDeviceSynchronize makes every capture in the process
 // invalid, cudaFree none that another thread (or, in relaxed mode, this one) has under way.  5 us on an idle device; 700
 // without the anchor.
-bool device_idle() {
+static bool device_idle() {
     void* p = nullptr;
     if (cudaMalloc(&p, 4) != cudaSuccess) return false;
     return cudaFree(p) == cudaSuccess;
@@ -673,6 +676,8 @@ bool expert_free(void* p, bool pooled, int device) {
     if (now != device) ok = cudaSetDevice(now) == cudaSuccess && ok;
     return ok;
 }
+
+namespace {
 
 moqe_status check_format(int N, int K, int bits, int group) {
     if (N <= 0 || K <= 0) return MOQE_ERR_SHAPE;
