@@ -8,12 +8,13 @@
 // 32 bytes of a row, so a k-block of 128 bytes a row is four instructions of about the same duration, whatever the format, and is
 // the unit that work is split by.
 //
-// One CTA to an SM.  Warp 4 (one lane) fills a ring of stages with bulk copies (weights with their scales: one copy; token rows:
-// one; their scales: one), warp 5 (one elected lane) copies scales to tensor memory and issues the MMAs into one of two
-// accumulators, warps 0-3 read the other one, a thread a channel, scale, round and store.  Work: whole tiles dealt out in turn where
-// there are plenty; else the tiles' k-blocks in one sequence, an equal share to every CTA ("stream-K").  A warp that holds part
-// of a tile parks its fp32 sums and counts itself in; the last one adds them up in the order of the CTAs, so that a call gives
-// the same bits every time.  Nobody waits for another CTA.
+// One CTA to an SM.  Two warps (one lane each) fill a ring of stages with bulk copies: weights with their scales (one copy), which
+// do not wait for the kernel that quantizes the rows; token rows and their scales (two).  One warp (one elected lane) copies scales
+// to tensor memory and issues the MMAs into one of two accumulators; eight warps read the other one, a thread a channel, scale,
+// round and store.  Work: whole tiles dealt out in turn where there are plenty; else, and for what is left over, the tiles' k-blocks
+// in one sequence, an equal share to every worker ("stream-K").  A warp that holds part of a tile parks its fp32 sums and counts
+// itself in; the last one adds them up in the order of the workers, so that a call gives the same bits every time.  Nobody waits
+// for another worker.
 //
 // Every mbarrier wait is bounded; on expiry the CTA raises its abort flag, latches MOQE_ERR_TIMEOUT, lets copies in flight land,
 // frees its tensor memory and returns.
@@ -23,13 +24,23 @@
 namespace moqe {
 namespace {
 
-constexpr int FP_TN = 128;                       // most tokens of a tile
-constexpr int FP_THREADS = 192;
+constexpr int FP_BAND = 8;                       // token tiles that are gone through together (see FpWalk)
+constexpr int FP_EPI_WARPS = 8;
+constexpr int FP_WEIGHTS_WARP = FP_EPI_WARPS, FP_MMA_WARP = FP_EPI_WARPS + 1, FP_TOKENS_WARP = FP_EPI_WARPS + 2;
+constexpr int FP_THREADS = 32 * (FP_EPI_WARPS + 3);
 constexpr int FP_MAX_STAGES = 12;
-constexpr int FP_RING_BYTES = 216 * 1024;
-constexpr int FP_SMEM = FP_RING_BYTES + 1024;
-constexpr int FP_SF_COLS = 32;                   // tensor-memory columns of a k-block's scales: weights' 16, tokens' 16
-constexpr int FP_SF_COL0 = 2 * FP_TN;            // two of them behind the accumulators
+constexpr int FP_RING_BYTES = 200 * 1024;
+constexpr int FP_BOX = 32 * 64;                  // 32 tokens x 32 channels of bf16, an epilogue warp's
+constexpr int FP_SMEM = FP_RING_BYTES + FP_EPI_WARPS * FP_BOX + 1024;
+
+// CG: SMs to a tile.  Tensor memory: two accumulators, then as many sets of scales as the ring has stages (a set: the weights'
+// columns, four to 128 k (MXFP4) or 64 k (NVFP4), then the tokens', four or eight).  A pair's accumulators of 256 columns leave too
+// little room for that: the second one begins half way through the first, and whoever reads an accumulator reads the shared half
+// first; and there are two sets for NVFP4.
+template <int CG> struct FpCfg {
+    static constexpr int ACC1 = 128;                 // column of the second accumulator
+    static constexpr int SF0 = 128 * (CG + 1);       // column of the scales
+};
 
 struct FpGemmExpert { const uint8_t* tiles; const float* outer; int format, KB; };
 struct FpGemmParams {
@@ -37,17 +48,20 @@ struct FpGemmParams {
     const int32_t *perm, *offsets;
     FpTokens t;
     uint32_t* counters;          // [CTA][warp], zero on entry
-    float* partials;             // [CTA][2][TN][128]
+    uint4* partials;             // [CTA][2][TN / 4][128]: four tokens' fp32 sums of a channel
     __nv_bfloat16* Y;
     int* status;
-    int E, N, NT, TN;            // channel tiles; tokens of a tile
+    int E, N, NT, TN;            // NT: tiles of 128 channels; TN: tokens of a tile
     int stages, stage_bytes, b_off, sfb_off;
+    int split_cost, least_share;     // what splitting costs, and the least share of a worker, in k-blocks
 };
 
 struct FpSched {
-    int off[MOQE_MAX_EXPERTS + 1], tile0[MOQE_MAX_EXPERTS + 1], unit0[MOQE_MAX_EXPERTS + 1];
-    int KB[MOQE_MAX_EXPERTS], pad0[MOQE_MAX_EXPERTS];
-    int E, G, split;             // G: CTAs that share the split
+    // by place in the order of work: 4-bit experts first, then the bf16 ones, whose tiles are four times as deep
+    int order[MOQE_MAX_EXPERTS], tile0[MOQE_MAX_EXPERTS + 1], unit0[MOQE_MAX_EXPERTS + 1], KB[MOQE_MAX_EXPERTS], tts[MOQE_MAX_EXPERTS];
+    int off[MOQE_MAX_EXPERTS + 1], pad0[MOQE_MAX_EXPERTS];      // by expert
+    int W, NT;                   // workers (CTAs or pairs); channel tiles of a worker
+    int whole, u0, R, G;         // tiles dealt out whole; then R k-blocks from u0 on in equal shares for G workers
     uint32_t tmem;
     int abort;
 };
@@ -55,90 +69,203 @@ struct FpSched {
 // k-blocks [kb0, kb1) of channel tile nt of the tokens [i0, i0 + rows) of expert e
 struct FpPiece { int e, nt, i0, rows, kb0, kb1, KB; };
 
-// what one CTA does, piece after piece; every role walks it for itself
+// What one worker does, piece after piece; every role walks it for itself.  Tiles lie in bands of FP_BAND token tiles, in a band
+// channel tile by channel tile, so that the workers of a moment share both token and weight tiles in L2.  Whole tiles go to the
+// workers in turn; the rest are one sequence of k-blocks, cut into equal shares.
 struct FpWalk {
-    int e, t, u, ue;
-    __device__ __forceinline__ void start(const FpSched& s) {
-        e = 0;
-        const int c = blockIdx.x, U = s.unit0[s.E];
-        t = c;
+    int at, t, u, ue;
+    __device__ __forceinline__ void start(const FpSched& s, int w) {
+        at = 0;
+        t = w;
         u = ue = 0;
-        if (s.split && c < s.G) { u = (int)((long long)c * U / s.G); ue = (int)((long long)(c + 1) * U / s.G); }
+        if (w < s.G) { u = s.u0 + (int)((long long)w * s.R / s.G); ue = s.u0 + (int)((long long)(w + 1) * s.R / s.G); }
     }
     __device__ __forceinline__ bool next(const FpSched& s, const FpGemmParams& p, FpPiece& pc) {
         int tile;
-        if (s.split) {
-            if (u >= ue) return false;
-            while (u >= s.unit0[e + 1]) ++e;
-            const int v = u - s.unit0[e], KB = s.KB[e];
-            tile = v / KB;
-            pc.kb0 = v - tile * KB;
-            pc.kb1 = min(KB, pc.kb0 + ue - u);
-            u += pc.kb1 - pc.kb0;
-        } else {
-            if (t >= s.tile0[s.E]) return false;
-            while (t >= s.tile0[e + 1]) ++e;
-            tile = t - s.tile0[e];
+        if (t < s.whole) {
+            while (t >= s.tile0[at + 1]) ++at;
+            tile = t - s.tile0[at];
+            pc.KB = s.KB[at];
             pc.kb0 = 0;
-            pc.kb1 = s.KB[e];
-            t += gridDim.x;
+            pc.kb1 = pc.KB;
+            t += s.W;
+        } else {
+            if (u >= ue) return false;
+            while (u >= s.unit0[at + 1]) ++at;
+            const int v = u - s.unit0[at];
+            pc.KB = s.KB[at];
+            tile = v / pc.KB;
+            pc.kb0 = v - tile * pc.KB;
+            pc.kb1 = min(pc.KB, pc.kb0 + ue - u);
+            u += pc.kb1 - pc.kb0;
         }
-        const int tt = tile / p.NT;
-        pc.e = e;
-        pc.KB = s.KB[e];
-        pc.nt = tile - tt * p.NT;
-        pc.i0 = tt * p.TN;
-        pc.rows = min(p.TN, s.off[e + 1] - s.off[e] - pc.i0);
+        pc.e = s.order[at];
+        const int band = tile / (FP_BAND * s.NT), in = tile - band * FP_BAND * s.NT, deep = min(FP_BAND, s.tts[at] - band * FP_BAND);
+        pc.nt = in / deep;
+        pc.i0 = (band * FP_BAND + in - pc.nt * deep) * p.TN;
+        pc.rows = min(p.TN, s.off[pc.e + 1] - s.off[pc.e] - pc.i0);
         return true;
     }
 };
 
-// ---------------------------------------------------------------------------- PTX of the block-scaled forms
-// 128 rows x 4 scales, 512 bytes of shared memory, to four columns of tensor memory (32 lanes, repeated for every quarter)
-__device__ __forceinline__ void tmem_copy_scales(uint32_t taddr, uint32_t smem_addr) {
-    const uint64_t desc = (uint64_t)((smem_addr >> 4) & 0x3FFFu) | (8ull << 32) | (1ull << 46);    // rows of 16 bytes, eight to 128 bytes
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+// ---------------------------------------------------------------------------- PTX of the block-scaled and two-SM forms
+template <int CG>
+__device__ __forceinline__ void fp_tmem_alloc(uint32_t smem_dst) {
+    if constexpr (CG == 1) tmem_alloc(smem_dst, 512);
+    else {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_dst) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
 }
-template <int FORMAT>
+template <int CG>
+__device__ __forceinline__ void fp_tmem_dealloc(uint32_t taddr) {
+    if constexpr (CG == 1) tmem_dealloc(taddr, 512);
+    else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(taddr) : "memory");
+}
+// 128 rows x 4 scales, 512 bytes of shared memory, to four columns of tensor memory (32 lanes, repeated for every quarter); in both
+// CTAs of a pair, each from its own shared memory
+template <int CG>
+__device__ __forceinline__ void tmem_copy_scales(uint32_t taddr, uint64_t desc) {
+    if constexpr (CG == 1) asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+    else asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+#define MOQE_UMMA_FP4(GROUP, VEC)                                                                                              \
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"                                                             \
+                 "tcgen05.mma.cta_group::" GROUP ".kind::mxf4nvf4.block_scale.scale_vec::" VEC " [%0], %1, %2, %3, [%4], [%5], p;\n\t}" \
+                 ::"r"(d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory")
+template <int CG, int FORMAT>
 __device__ __forceinline__ void umma_fp4(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
-    if constexpr (FORMAT == MOQE_FP_MXFP4)
-        asm volatile(
-            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
-            "tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-            ::"r"(d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
-    else
-        asm volatile(
-            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
-            "tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-            ::"r"(d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+    if constexpr (FORMAT == MOQE_FP_MXFP4) {
+        if constexpr (CG == 1) MOQE_UMMA_FP4("1", "2X"); else MOQE_UMMA_FP4("2", "2X");
+    } else {
+        if constexpr (CG == 1) MOQE_UMMA_FP4("1", "4X"); else MOQE_UMMA_FP4("2", "4X");
+    }
 }
-// e2m1 x e2m1 -> fp32, both K-major, M = 128, N = n; scales E8M0 (bit 23) or e4m3; `id`: which of a column's four scales come first
+#undef MOQE_UMMA_FP4
+template <int CG>
+__device__ __forceinline__ void fp_umma_bf16(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    if constexpr (CG == 1) umma_bf16(d, adesc, bdesc, idesc, accumulate);
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+// arrives at the barrier (of both CTAs) when every MMA issued so far is done
+template <int CG>
+__device__ __forceinline__ void fp_commit(uint32_t bar) {
+    if constexpr (CG == 1) umma_commit(bar);
+    else {
+        const uint16_t both = 3;
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"(both) : "memory");
+    }
+}
+// e2m1 x e2m1 -> fp32, both K-major, M = 128 CG, N = n; scales E8M0 (bit 23) or e4m3; `id`: which of a column's four scales come first
+template <int CG>
 __device__ __forceinline__ uint32_t idesc_fp4(int n, bool e8m0, uint32_t id) {
-    return (id << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)e8m0 << 23) | ((128u >> 4) << 24) | (id << 29);
+    return (id << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)e8m0 << 23) | ((128u * CG >> 4) << 24) | (id << 29);
+}
+template <int CG>
+__device__ __forceinline__ uint32_t idesc_bf16(int n) {
+    return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((128u * CG >> 4) << 24);
 }
 
-// the MMAs of one k-block; sf: its tensor-memory columns
-template <int FORMAT>
-__device__ __forceinline__ void issue_kblock(uint32_t d, uint32_t a, uint32_t sfa, uint32_t b, uint32_t sfb, uint32_t sf, int n, int steps, bool first) {
-    const uint64_t ad = umma_desc_sw128(a), bd = umma_desc_sw128(b);
+// Two barriers' bounded wait: both tries are on their way before the first is looked at.
+__device__ __forceinline__ bool mbar_wait_two(uint32_t bar0, uint32_t parity0, uint32_t bar1, uint32_t parity1, volatile int* abort_flag, int* status) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 q, [%3], %4;\n\t"
+        "and.pred p, p, q;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(bar0), "r"(parity0), "r"(bar1), "r"(parity1) : "memory");
+    if (ok) return true;
+    bool got = mbar_wait_short(bar0, parity0, abort_flag, status);
+    got &= mbar_wait_short(bar1, parity1, abort_flag, status);
+    return got;
+}
+
+// The issuing warp's state, and the k-blocks of one piece.  A turn of the loop costs its instructions' latencies (waits, the elected
+// lane's branch, operands moved to the uniform datapath), so it holds nothing that can be worked out before it.  One SM's tiles
+// are small: two k-blocks to a turn there.  A pair multiplies 256 tokens in 512 cycles or more, and would rather have its stages back.
+// A wait that runs out is looked at after the piece: what is issued until then stays in bounds, and no later wait takes long.
+struct FpIssue {
+    Ring ring, last;             // the next stage; the last one (issued before it)
+    Ring behind;                 // the stage whose k-block had the next set of scales
+    int format, set, fresh;      // of the scales in tensor memory: their format, the next set of columns, sets that nobody has had yet
+    bool ok;
+};
+template <int CG, int FORMAT>
+__device__ __forceinline__ void issue_kblock(uint32_t d, uint32_t a, uint32_t b_off, uint32_t sfb_off, uint32_t sf, uint32_t id0, int n, bool first) {
+    constexpr int GROUPS = FORMAT == MOQE_FP_MXFP4 ? 2 : 4;
+    constexpr uint32_t GROUP = CG == 2 ? 8 : 4;                                             // columns of a group of the tokens' scales
+    constexpr uint32_t SECOND = (2u << 4) | (2u << 29);                                     // the second pair of a column's scales
+    const uint64_t ad = umma_desc_sw128(0) + (a >> 4), bd = ad + (b_off >> 4);
     if constexpr (FORMAT == MOQE_FP_BF16) {
-        const uint32_t id = umma_idesc(n);
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
-            if (s < steps) umma_bf16(d, ad + 2 * s, bd + 2 * s, id, first && s == 0 ? 0u : 1u);
+        for (int s = 0; s < 4; ++s) fp_umma_bf16<CG>(d, ad + 2 * s, bd + 2 * s, id0, first && s == 0 ? 0u : 1u);
     } else {
-        constexpr int GROUPS = FORMAT == MOQE_FP_MXFP4 ? 2 : 4;
+        // scales: rows of 16 bytes, eight to 128 bytes
+        const uint64_t sd = ((8ull << 32) | (1ull << 46)) + ((a + 16384) >> 4), td = ((8ull << 32) | (1ull << 46)) + ((a + sfb_off) >> 4);
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g) {
-            tmem_copy_scales(sf + 4 * g, sfa + 512 * g);
-            tmem_copy_scales(sf + 16 + 4 * g, sfb + 512 * g);
+            tmem_copy_scales<CG>(sf + 4 * g, sd + 32 * g);
+            tmem_copy_scales<CG>(sf + 4 * GROUPS + GROUP * g, td + 32 * g);
+            if (CG == 2 && n > 128) tmem_copy_scales<CG>(sf + 4 * GROUPS + GROUP * g + 4, td + 32 * (GROUPS + g));
         }
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
             const int g = FORMAT == MOQE_FP_MXFP4 ? s >> 1 : s;
-            const uint32_t id = idesc_fp4(n, FORMAT == MOQE_FP_MXFP4, FORMAT == MOQE_FP_MXFP4 ? (s & 1) * 2 : 0);
-            if (s < steps) umma_fp4<FORMAT>(d, ad + 2 * s, bd + 2 * s, id, sf + 4 * g, sf + 16 + 4 * g, first && s == 0 ? 0u : 1u);
+            umma_fp4<CG, FORMAT>(d, ad + 2 * s, bd + 2 * s, FORMAT == MOQE_FP_MXFP4 && (s & 1) ? id0 | SECOND : id0, sf + 4 * g,
+                                 sf + 4 * GROUPS + GROUP * g, first && s == 0 ? 0u : 1u);
         }
+    }
+}
+template <int CG, int FORMAT>
+__device__ __forceinline__ void issue_piece(FpIssue& q, const FpGemmParams& p, uint32_t ring0, uint32_t bar_full, uint32_t bar_empty, uint32_t d,
+                                            uint32_t sf0, int n, int kblocks, uint32_t accfull, volatile int* abort_flag) {
+    constexpr uint32_t SET = (FORMAT == MOQE_FP_MXFP4 ? 2 : 4) * (CG == 2 ? 12 : 8);        // columns of a set
+    // With as many sets as stages, a stage that has been filled again frees its set.  A pair has room for two of NVFP4's.
+    constexpr bool SCARCE = CG == 2 && FORMAT == MOQE_FP_NVFP4;
+    constexpr int TURN = CG == 2 ? 1 : 2;
+    const int sets = SCARCE ? 2 : p.stages;
+    const uint32_t id0 = FORMAT == MOQE_FP_BF16 ? idesc_bf16<CG>(n) : idesc_fp4<CG>(n, FORMAT == MOQE_FP_MXFP4, 0);
+    if (FORMAT != MOQE_FP_BF16 && q.format != FORMAT) {
+        // sets of another size: everything before must have been multiplied
+        if (q.format != 0) q.ok &= mbar_wait_short(bar_empty + 8 * q.last.stage, q.last.phase, abort_flag, p.status);
+        q.format = FORMAT;
+        q.set = 0;
+        q.fresh = sets;
+        q.behind = q.ring;
+    }
+    for (int k = 0; k < kblocks; k += TURN) {
+        const Ring r0 = q.ring;
+        Ring r1 = r0;
+        r1.advance(p.stages);
+        const bool two = TURN == 2 && k + 1 < kblocks;
+        const uint32_t full0 = bar_full + 8 * r0.stage, full1 = bar_full + 8 * r1.stage;
+        if constexpr (SCARCE) {
+            if (q.fresh > 0) --q.fresh;
+            else { q.ok &= mbar_wait_short(bar_empty + 8 * q.behind.stage, q.behind.phase, abort_flag, p.status); q.behind.advance(p.stages); }
+        }
+        q.ok &= two ? mbar_wait_two(full0, r0.phase, full1, r1.phase, abort_flag, p.status) : mbar_wait_short(full0, r0.phase, abort_flag, p.status);
+        __syncwarp();
+        tc_fence_after();
+        const uint32_t a0 = ring0 + r0.stage * p.stage_bytes, a1 = ring0 + r1.stage * p.stage_bytes;
+        const int set1 = q.set + 1 == sets ? 0 : q.set + 1;
+        if (elect_one()) {
+            issue_kblock<CG, FORMAT>(d, a0, p.b_off, p.sfb_off, sf0 + q.set * SET, id0, n, k == 0);
+            fp_commit<CG>(bar_empty + 8 * r0.stage);
+            if (two) {
+                issue_kblock<CG, FORMAT>(d, a1, p.b_off, p.sfb_off, sf0 + set1 * SET, id0, n, false);
+                fp_commit<CG>(bar_empty + 8 * r1.stage);
+            }
+            if (k + TURN >= kblocks) fp_commit<CG>(accfull);
+        }
+        __syncwarp();
+        q.last = two ? r1 : r0;
+        q.ring = q.last;
+        q.ring.advance(p.stages);
+        q.set = !two ? set1 : set1 + 1 == sets ? 0 : set1 + 1;
     }
 }
 
@@ -147,220 +274,349 @@ __device__ __forceinline__ uint32_t count_in(uint32_t* p) {
     asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(old) : "l"(p) : "memory");
     return old;
 }
-
-// 32 tokens' sums of this lane's channel -> Y.  Lanes of a pair swap halves, so that each stores two channels of every other token.
-// (N is even and the pair's first channel n & ~1 too.)
-__device__ __forceinline__ void store_columns(const FpGemmParams& p, const float (&v)[32], int to, int cols, int n, int lane) {
-    const int odd = lane & 1;
-    __nv_bfloat16* y = p.Y + (n & ~1);
-#pragma unroll
-    for (int c = 0; c < 32; c += 2) {
-        const float give = odd ? v[c] : v[c + 1], keep = odd ? v[c + 1] : v[c];
-        const float got = __shfl_xor_sync(0xFFFFFFFFu, give, 1);
-        const int row = __shfl_sync(0xFFFFFFFFu, to, c + odd);
-        const __nv_bfloat162 h = odd ? __floats2bfloat162_rn(got, keep) : __floats2bfloat162_rn(keep, got);
-        if (c + odd < cols && n < p.N) *reinterpret_cast<__nv_bfloat162*>(y + (size_t)row * p.N) = h;
-    }
+__device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ uint32_t of_leader(uint32_t addr) {       // the same place in the pair's first CTA
+    uint32_t d;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(d) : "r"(addr));
+    return d;
+}
+__device__ __forceinline__ void leader_arrive(uint32_t cluster_addr) {
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
 }
 
+// An epilogue warp holds 32 channels x 32 tokens of sums as the 16-row shape of tensor-memory loads gives them: token block j (eight
+// tokens), channel half h: v[16 h + 4 j + {0, 1}] = channel 16 h + lane / 4, tokens 8 j + 2 (lane % 4) + {0, 1}; + {2, 3}: channel + 8.
+// So pairs of tokens are packed in a thread, and a transposing matrix store puts eight channels of a token side by side.
+__device__ __forceinline__ void tmem_ld_16x256(uint32_t taddr, uint32_t* v) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+          "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+// Scaled (by channel, w, and token, x of token `lane`) and rounded: o[4 j + b] = tokens 8 j + 2 (lane % 4) + {0, 1} of channel 8 b + lane / 4.
+__device__ __forceinline__ void pack_block(const uint32_t* v, bool scaled, const float (&w)[4], float x, int lane, uint32_t* o) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        float x0 = 1.f, x1 = 1.f;
+        if (scaled) { x0 = __shfl_sync(0xFFFFFFFFu, x, 8 * j + 2 * (lane & 3)); x1 = __shfl_sync(0xFFFFFFFFu, x, 8 * j + 2 * (lane & 3) + 1); }
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            float lo = __uint_as_float(v[16 * (b >> 1) + 4 * j + 2 * (b & 1)]), hi = __uint_as_float(v[16 * (b >> 1) + 4 * j + 2 * (b & 1) + 1]);
+            if (scaled) { lo *= w[b] * x0; hi *= w[b] * x1; }
+            o[4 * j + b] = pack_bf16(lo, hi);
+        }
+    }
+}
+// `cols` tokens of them -> Y, through the warp's box of shared memory (64 bytes a token; chunks permuted so that neither side has
+// bank conflicts).  to: the row of Y of token `lane`; n0: the first channel.  (N is a multiple of 8, so a 16-byte chunk is there or not.)
+__device__ __forceinline__ void store_block(const FpGemmParams& p, const uint32_t* o, uint32_t box, int to, int cols, int n0, int lane) {
+    const uint32_t put = box + (lane & 7) * 64 + (((lane >> 3) ^ ((lane >> 1) & 3)) << 4);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};"
+                     ::"r"(put + j * 512), "r"(o[4 * j]), "r"(o[4 * j + 1]), "r"(o[4 * j + 2]), "r"(o[4 * j + 3]) : "memory");
+    __syncwarp();
+    const int tok = lane >> 2, chunk = lane & 3, n = n0 + chunk * 8;
+    const uint32_t get = box + tok * 64 + ((chunk ^ ((tok >> 1) & 3)) << 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint4 q;
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "r"(get + i * 512));
+        const int row = __shfl_sync(0xFFFFFFFFu, to, tok + 8 * i);
+        if (tok + 8 * i < cols && n < p.N) *reinterpret_cast<uint4*>(p.Y + (size_t)row * p.N + n) = q;
+    }
+    __syncwarp();
+}
+
+template <int CG>
 __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_constant__ FpGemmParams p) {
+    using L = FpCfg<CG>;
     extern __shared__ unsigned char smem_raw[];
     __shared__ FpSched sh;
     __shared__ unsigned long long bars[2 * FP_MAX_STAGES + 4];
     const uint32_t ring0 = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = CG == 2 ? cluster_rank() : 0u;
+    const int worker = blockIdx.x / CG;
     const uint32_t bar_full = smem_u32(bars), bar_empty = bar_full + 8 * FP_MAX_STAGES;
     const uint32_t bar_accfull = bar_empty + 8 * FP_MAX_STAGES, bar_accempty = bar_accfull + 16;
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < p.stages; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
-        for (int i = 0; i < 2; ++i) { mbar_init(bar_accfull + 8 * i, 1); mbar_init(bar_accempty + 8 * i, 128); }
+        // (weights and tokens arrive on their own; a pair's first CTA issues the MMAs: its full barriers take an arrival for the other CTA, too)
+        for (int i = 0; i < p.stages; ++i) { mbar_init(bar_full + 8 * i, CG == 2 && rank == 0 ? 3 : 2); mbar_init(bar_empty + 8 * i, 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(bar_accfull + 8 * i, 1); mbar_init(bar_accempty + 8 * i, FP_EPI_WARPS * CG); }
         sh.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 5) tmem_alloc(smem_u32(&sh.tmem), 512);
-    if (warp == 4) {
+    if (warp == FP_MMA_WARP) fp_tmem_alloc<CG>(smem_u32(&sh.tmem));
+    if (warp == FP_WEIGHTS_WARP) {
         // the schedule, from the sort's offset table (the kernel before this one waited for it before it let this one start)
-        const bool is = lane < p.E;
-        const int lo = is ? __ldcg(p.offsets + lane) : 0, hi = is ? __ldcg(p.offsets + lane + 1) : 0;
-        const int rows = hi - lo, KB = is ? p.ex[lane].KB : 1;
-        const int tiles = (rows + p.TN - 1) / p.TN * p.NT;
-        int pad = (rows + 127) & ~127, tsum = tiles, usum = tiles * KB, psum = pad;
+        {
+            const bool is = lane < p.E, deep = is && p.ex[lane].format == MOQE_FP_BF16;
+            const int lo = is ? __ldcg(p.offsets + lane) : 0, hi = is ? __ldcg(p.offsets + lane + 1) : 0;
+            const uint32_t bf = __ballot_sync(0xFFFFFFFFu, deep), four = __ballot_sync(0xFFFFFFFFu, is && !deep), below = (1u << lane) - 1u;
+            int psum = (hi - lo + 127) & ~127;
+            const int pad = psum;
 #pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int a = __shfl_up_sync(0xFFFFFFFFu, tsum, d), b = __shfl_up_sync(0xFFFFFFFFu, usum, d), c = __shfl_up_sync(0xFFFFFFFFu, psum, d);
-            if (lane >= d) { tsum += a; usum += b; psum += c; }
+            for (int d = 1; d < 32; d <<= 1) {
+                const int c = __shfl_up_sync(0xFFFFFFFFu, psum, d);
+                if (lane >= d) psum += c;
+            }
+            if (is) {
+                sh.off[lane] = lo;
+                sh.pad0[lane] = psum - pad;
+                if (lane == p.E - 1) sh.off[p.E] = hi;
+                sh.order[deep ? __popc(four) + __popc(bf & below) : __popc(four & below)] = lane;
+            }
         }
-        if (is) {
-            sh.off[lane] = lo; sh.KB[lane] = KB; sh.pad0[lane] = psum - pad;
-            sh.tile0[lane] = tsum - tiles; sh.unit0[lane] = usum - tiles * KB;
-            if (lane == p.E - 1) { sh.off[p.E] = hi; sh.tile0[p.E] = tsum; sh.unit0[p.E] = usum; }
-        }
-        const int T = __shfl_sync(0xFFFFFFFFu, tsum, 31), U = __shfl_sync(0xFFFFFFFFu, usum, 31);
-        if (lane == 0) {
-            sh.E = p.E;
-            sh.split = T < 2 * (int)gridDim.x;
-            sh.G = max(1, min((int)gridDim.x, U / 4));
+        __syncwarp();
+        {
+            const bool is = lane < p.E;
+            const int e = is ? sh.order[lane] : 0, rows = is ? sh.off[e + 1] - sh.off[e] : 0, KB = is ? p.ex[e].KB : 1, NT = (p.NT + CG - 1) / CG;
+            const int tts = (rows + p.TN - 1) / p.TN, tiles = tts * NT;
+            int tsum = tiles, usum = tiles * KB;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int a = __shfl_up_sync(0xFFFFFFFFu, tsum, d), b = __shfl_up_sync(0xFFFFFFFFu, usum, d);
+                if (lane >= d) { tsum += a; usum += b; }
+            }
+            if (is) {
+                sh.tile0[lane] = tsum - tiles; sh.unit0[lane] = usum - tiles * KB; sh.KB[lane] = KB; sh.tts[lane] = tts;
+                if (lane == p.E - 1) { sh.tile0[p.E] = tsum; sh.unit0[p.E] = usum; }
+            }
+            // Rounds of whole tiles; what does not fill a round, and the round before it, are split if that saves more k-blocks than
+            // parking and adding up cost.
+            const int T = __shfl_sync(0xFFFFFFFFu, tsum, 31), U = __shfl_sync(0xFFFFFFFFu, usum, 31), W = (int)gridDim.x / CG;
+            const uint32_t some = __ballot_sync(0xFFFFFFFFu, tiles > 0);
+            const int left = T % W, KBlast = __shfl_sync(0xFFFFFFFFu, KB, some ? 31 - __clz(some) : 0);
+            int whole = T;
+            if (left != 0 && (long long)KBlast * (W - left) > (long long)p.split_cost * W) whole = T < W ? 0 : T - left - W;
+            const uint32_t holds = __ballot_sync(0xFFFFFFFFu, is && whole >= tsum - tiles && whole < tsum);
+            const int at = holds ? __ffs(holds) - 1 : 0;
+            const int u0 = whole < T ? __shfl_sync(0xFFFFFFFFu, usum - tiles * KB + (whole - (tsum - tiles)) * KB, at) : U;
+            if (lane == 0) {
+                sh.W = W; sh.NT = NT; sh.whole = whole; sh.u0 = u0; sh.R = U - u0;
+                sh.G = U > u0 ? max(1, min(W, (U - u0) / p.least_share)) : 0;
+            }
         }
     }
     tc_fence_before();
     __syncthreads();
+    if constexpr (CG == 2) cluster_sync();
     tc_fence_after();
     const uint32_t tmem = sh.tmem;
 
-    if (warp == 4) {
-        // ---------------- producer ----------------
+    if (warp == FP_WEIGHTS_WARP) {
+        // ---------------- weights and their scales ----------------
         if (lane == 0) {
             FpWalk walk;
             FpPiece pc;
             Ring ring;
             bool ok = true;
-            // The weights of the first stages are fetched while the kernel before is still writing the token rows.
-            auto weights = [&](const FpPiece& q, int kb, int st) {
-                const int format = p.ex[q.e].format, sfb = fp_sf_bytes(format), n16 = (q.rows + 15) & ~15;
-                const int stride = fp_tile_stride(format);
-                const uint32_t full = bar_full + 8 * st;
-                mbar_expect_tx(full, (uint32_t)(stride + n16 * 128 + sfb));
-                bulk_load(ring0 + st * p.stage_bytes, p.ex[q.e].tiles + ((size_t)q.nt * q.KB + kb) * stride, stride, full);
-            };
-            auto tokens = [&](const FpPiece& q, int kb, int st) {
-                const int format = p.ex[q.e].format, sfb = fp_sf_bytes(format), n16 = (q.rows + 15) & ~15;
-                const uint32_t full = bar_full + 8 * st, base = ring0 + st * p.stage_bytes;
-                const size_t pad0 = sh.pad0[q.e];
-                const int seg = (sh.off[q.e + 1] - sh.off[q.e] + 127) & ~127;
-                const uint8_t* codes = p.t.codes + pad0 * p.t.row_bytes + ((size_t)kb * seg + q.i0) * 128;
-                bulk_load(base + p.b_off, codes, n16 * 128, full);
-                if (sfb) bulk_load(base + p.sfb_off, p.t.sf + (pad0 >> 7) * p.t.block_sf + ((size_t)(q.i0 >> 7) * q.KB + kb) * sfb, sfb, full);
-            };
-            walk.start(sh);
-            int ahead = 0;
-            while (ahead < p.stages && walk.next(sh, p, pc))
-                for (int kb = pc.kb0; kb < pc.kb1 && ahead < p.stages; ++kb, ++ahead) weights(pc, kb, ahead);
-            asm volatile("griddepcontrol.wait;" ::: "memory");
-            asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-            asm volatile("fence.proxy.async;" ::: "memory");
-            int done = 0;
-            walk.start(sh);
+            walk.start(sh, worker);
             while (ok && walk.next(sh, p, pc)) {
-                for (int kb = pc.kb0; kb < pc.kb1; ++kb, ++done) {
-                    if (done >= ahead) {
-                        if (!(ok = mbar_wait_short(bar_empty + 8 * ring.stage, ring.phase ^ 1u, &sh.abort, p.status))) break;
-                        weights(pc, kb, ring.stage);
-                    }
-                    tokens(pc, kb, ring.stage);
+                const FpGemmExpert& x = p.ex[pc.e];
+                const uint32_t stride = fp_tile_stride(x.format);
+                const uint8_t* src = x.tiles + ((size_t)min(pc.nt * CG + (int)rank, p.NT - 1) * pc.KB + pc.kb0) * stride;
+                for (int k = pc.kb1 - pc.kb0; k > 0; --k, src += stride) {
+                    if (!(ok = mbar_wait_short(bar_empty + 8 * ring.stage, ring.phase ^ 1u, &sh.abort, p.status))) break;
+                    mbar_expect_tx(bar_full + 8 * ring.stage, stride);
+                    bulk_load(ring0 + ring.stage * p.stage_bytes, src, stride, bar_full + 8 * ring.stage);
                     ring.advance(p.stages);
                 }
             }
         }
         __syncwarp();
-    } else if (warp == 5) {
+    } else if (warp == FP_TOKENS_WARP) {
+        // ---------------- token rows (of a pair, each CTA's half) and their scales ----------------
+        if (lane == 0) {
+            FpWalk walk;
+            FpPiece pc;
+            Ring ring;
+            bool ok = true;
+            asm volatile("griddepcontrol.wait;" ::: "memory");
+            asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+            asm volatile("fence.proxy.async;" ::: "memory");
+            walk.start(sh, worker);
+            while (ok && walk.next(sh, p, pc)) {
+                const int sfb = fp_sf_bytes(p.ex[pc.e].format), n = (pc.rows + 15) & ~15, shift = p.t.sf_shift;
+                const size_t pad0 = sh.pad0[pc.e], seg = (sh.off[pc.e + 1] - sh.off[pc.e] + 127) & ~127;
+                const uint32_t bytes = n / CG * 128, sbytes = n > 128 ? 2 * sfb : sfb;
+                const size_t step = seg * 128, sstep = (seg >> shift) * sfb;
+                const uint8_t* src = p.t.codes + pad0 * p.t.row_bytes + pc.kb0 * step + (size_t)(pc.i0 + rank * (n / 2)) * 128;
+                const uint8_t* ssrc = p.t.sf + (pad0 >> shift) * p.t.block_sf + pc.kb0 * sstep + (size_t)(pc.i0 >> shift) * sfb;
+                for (int k = pc.kb1 - pc.kb0; k > 0; --k, src += step, ssrc += sstep) {
+                    if (!(ok = mbar_wait_short(bar_empty + 8 * ring.stage, ring.phase ^ 1u, &sh.abort, p.status))) break;
+                    const uint32_t full = bar_full + 8 * ring.stage, base = ring0 + ring.stage * p.stage_bytes;
+                    mbar_expect_tx(full, bytes + sbytes);
+                    bulk_load(base + p.b_off, src, bytes, full);
+                    if (sbytes) bulk_load(base + p.sfb_off, ssrc, sbytes, full);
+                    ring.advance(p.stages);
+                }
+            }
+        }
+        __syncwarp();
+    } else if (warp == FP_MMA_WARP && rank == 0) {
         // ---------------- MMA issuer: the whole warp walks, one elected lane issues ----------------
         FpWalk walk;
         FpPiece pc;
-        Ring ring;
-        bool ok = true;
-        uint32_t uses = 0, kbs = 0;
-        int last_stage = 0, last2_stage = 0;
-        uint32_t last_phase = 0, last2_phase = 0;
-        walk.start(sh);
-        while (ok && walk.next(sh, p, pc)) {
-            const int buf = uses & 1;
-            const int format = p.ex[pc.e].format, n = (pc.rows + 15) & ~15;
-            const uint32_t d = tmem + buf * FP_TN;
-            if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait_short(bar_accempty + 8 * buf, ((uses >> 1) & 1u) ^ 1u, &sh.abort, p.status)))) break;
-            for (int kb = pc.kb0; kb < pc.kb1; ++kb, ++kbs) {
-                // The scales' columns alternate: those of two k-blocks ago must have been multiplied.
-                if (format != MOQE_FP_BF16 && kbs >= 2) ok = mbar_wait_short(bar_empty + 8 * last2_stage, last2_phase, &sh.abort, p.status);
-                ok = ok && mbar_wait_short(bar_full + 8 * ring.stage, ring.phase, &sh.abort, p.status);
-                if (!(ok = __all_sync(0xFFFFFFFFu, ok))) break;
-                tc_fence_after();
-                const uint32_t a = ring0 + ring.stage * p.stage_bytes, b = a + p.b_off, sfb = a + p.sfb_off, sf = tmem + FP_SF_COL0 + (kbs & 1u) * FP_SF_COLS;
-                if (elect_one()) {
-                    if (format == MOQE_FP_MXFP4) issue_kblock<MOQE_FP_MXFP4>(d, a, a + 16384, b, sfb, sf, n, 4, kb == pc.kb0);
-                    else if (format == MOQE_FP_NVFP4) issue_kblock<MOQE_FP_NVFP4>(d, a, a + 16384, b, sfb, sf, n, 4, kb == pc.kb0);
-                    else issue_kblock<MOQE_FP_BF16>(d, a, 0, b, 0, 0, n, 4, kb == pc.kb0);
-                    umma_commit(bar_empty + 8 * ring.stage);
-                    if (kb + 1 == pc.kb1) umma_commit(bar_accfull + 8 * buf);
-                }
-                __syncwarp();
-                last2_stage = last_stage; last2_phase = last_phase;
-                last_stage = ring.stage; last_phase = ring.phase;
-                ring.advance(p.stages);
-            }
+        FpIssue q;
+        q.format = 0; q.set = 0; q.fresh = 0; q.ok = true;
+        uint32_t uses = 0;
+        const uint32_t sf0 = tmem + L::SF0;
+        walk.start(sh, worker);
+        while (q.ok && walk.next(sh, p, pc)) {
+            const int buf = uses & 1, format = p.ex[pc.e].format, n = (pc.rows + 15) & ~15;
+            // one SM: the accumulator of two tiles ago has been read; a pair: what this one shares with the last has
+            const uint32_t before = CG == 2 ? uses + 1 : uses, d = tmem + buf * L::ACC1, accfull = bar_accfull + 8 * buf;
+            q.ok = mbar_wait_short(bar_accempty + 8 * (before & 1), ((before >> 1) & 1u) ^ 1u, &sh.abort, p.status);
+            if (format == MOQE_FP_MXFP4) issue_piece<CG, MOQE_FP_MXFP4>(q, p, ring0, bar_full, bar_empty, d, sf0, n, pc.kb1 - pc.kb0, accfull, &sh.abort);
+            else if (format == MOQE_FP_NVFP4) issue_piece<CG, MOQE_FP_NVFP4>(q, p, ring0, bar_full, bar_empty, d, sf0, n, pc.kb1 - pc.kb0, accfull, &sh.abort);
+            else issue_piece<CG, MOQE_FP_BF16>(q, p, ring0, bar_full, bar_empty, d, sf0, n, pc.kb1 - pc.kb0, accfull, &sh.abort);
+            q.ok = __all_sync(0xFFFFFFFFu, q.ok);
             ++uses;
         }
+    } else if (warp == FP_MMA_WARP) {
+        // ---------------- a pair's second CTA: tells the first when its half of a stage has landed ----------------
+        if (lane == 0) {
+            FpWalk walk;
+            FpPiece pc;
+            Ring ring;
+            bool ok = true;
+            const uint32_t to = of_leader(bar_full);
+            walk.start(sh, worker);
+            while (ok && walk.next(sh, p, pc)) {
+                for (int kb = pc.kb0; kb < pc.kb1; ++kb) {
+                    if (!(ok = mbar_wait_short(bar_full + 8 * ring.stage, ring.phase, &sh.abort, p.status))) break;
+                    leader_arrive(to + 8 * ring.stage);
+                    ring.advance(p.stages);
+                }
+            }
+        }
+        __syncwarp();
     } else {
-        // ---------------- epilogue: thread = channel = TMEM lane ----------------
+        // ---------------- epilogue: thread = channel = TMEM lane; two warps to a quarter of the lanes, 64 tokens at a time ----------------
         asm volatile("griddepcontrol.wait;" ::: "memory");
+        const int quarter = warp & 3, half = warp >> 2;
+        const uint32_t box = ring0 + FP_RING_BYTES + warp * FP_BOX;
+        const uint32_t accempty = CG == 2 ? of_leader(bar_accempty) : bar_accempty;
         FpWalk walk;
         FpPiece pc;
         bool ok = true;
         uint32_t uses = 0;
-        walk.start(sh);
+        walk.start(sh, worker);
         while (ok && walk.next(sh, p, pc)) {
             const int buf = uses & 1;
-            const int j0 = sh.off[pc.e] + pc.i0, n = pc.nt * 128 + warp * 32 + lane;
+            const int j0 = sh.off[pc.e] + pc.i0, n0 = (pc.nt * CG + (int)rank) * 128 + quarter * 32;
             const float* ow = p.ex[pc.e].outer;
             const float* ox = p.t.outer + sh.pad0[pc.e] + pc.i0;
-            const float w = ow ? ow[n] : 1.f;
+            float w[4];                                      // channel scales of this lane's rows
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { const int n = n0 + (lane >> 2) + 8 * i; w[i] = ow && n < p.N ? ow[n] : 1.f; }
+            // where this lane's share of the tokens goes, and their scales: fetched while the tile is multiplied
+            int to[CG][2];
+            float sx[CG][2];
+#pragma unroll
+            for (int g = 0; g < CG; ++g)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int c = g * 128 + half * 64 + h * 32 + lane;
+                    to[g][h] = c < pc.rows ? p.perm[j0 + c] : 0;
+                    sx[g][h] = ow && c < pc.rows ? ox[c] : 1.f;
+                }
             if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait_short(bar_accfull + 8 * buf, (uses >> 1) & 1u, &sh.abort, p.status)))) break;
             tc_fence_after();
-            const uint32_t acc = tmem + ((uint32_t)(warp * 32) << 16) + buf * FP_TN;
+            const uint32_t acc = tmem + ((uint32_t)(quarter * 32) << 16) + buf * L::ACC1;
             const bool whole = pc.kb0 == 0 && pc.kb1 == pc.KB;
-            int c0 = blockIdx.x, c1 = blockIdx.x;
-            bool finish = true;
-            if (!whole) {
-                // the CTAs that share this tile
-                const long long U = sh.unit0[sh.E], G = sh.G;
-                const long long first = walk.u - pc.kb1, last = first + pc.KB - 1;
-                c0 = (int)(((first + 1) * G - 1) / U);
-                c1 = (int)(((last + 1) * G - 1) / U);
-                float* slot = p.partials + ((size_t)blockIdx.x * 2 + (pc.kb0 == 0 ? 1 : 0)) * p.TN * 128 + warp * 32 + lane;
-                for (int c = 0; c < pc.rows; c += 32) {
-                    uint32_t v[32];
-                    tmem_ld32(acc + c, v);
-                    tmem_ld_wait();
+            // parked sums: a CTA has a place for its last piece (the start of a tile) and one for its first
+            auto slot_of = [&](int w, bool starts) { return p.partials + ((size_t)(w * CG + rank) * 2 + (starts ? 1 : 0)) * p.TN * 32 + quarter * 32 + lane; };
+            uint4* slot = slot_of(worker, pc.kb0 == 0);
+            uint32_t o[16];                                  // 32 tokens, rounded
 #pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (c + i < pc.rows) __stcg(slot + (c + i) * 128, __uint_as_float(v[i]));
+            for (int g = 0; g < CG; ++g) {
+                // a pair's first turn: the half that the accumulators share, columns 128.. of the first, 0.. of the second
+                const bool upper = CG == 2 && (g ^ buf ^ 1);
+                const int c = (upper ? 128 : 0) + half * 64, cols = pc.rows - c;
+                uint32_t v[64];
+                if (cols > 0) { tmem_ld_16x256(acc + c, v); tmem_ld_16x256(acc + (16u << 16) + c, v + 16); }
+                if (cols > 32) { tmem_ld_16x256(acc + c + 32, v + 32); tmem_ld_16x256(acc + (16u << 16) + c + 32, v + 48); }
+                tmem_ld_wait();
+                if (g == 0) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) { if constexpr (CG == 2) leader_arrive(accempty + 8 * buf); else mbar_arrive(accempty + 8 * buf); }
                 }
+                if (whole) {
+                    if (cols > 0) {
+                        pack_block(v, ow != nullptr, w, upper ? sx[CG - 1][0] : sx[0][0], lane, o);
+                        store_block(p, o, box, upper ? to[CG - 1][0] : to[0][0], cols, n0, lane);
+                    }
+                    if (cols > 32) {
+                        pack_block(v + 32, ow != nullptr, w, upper ? sx[CG - 1][1] : sx[0][1], lane, o);
+                        store_block(p, o, box, upper ? to[CG - 1][1] : to[0][1], cols - 32, n0, lane);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {           // (token block i / 2, channel half i % 2)
+                        const int r = 32 * (i >> 3) + 16 * (i & 1) + 4 * ((i >> 1) & 3);
+                        if (8 * (i >> 1) < cols) __stcg(slot + (c >> 3) * 256 + i * 128, make_uint4(v[r], v[r + 1], v[r + 2], v[r + 3]));
+                    }
+                }
+            }
+            if (!whole) {
+                // the workers that share this tile
+                const long long R = sh.R, G = sh.G;
+                const long long first = walk.u - pc.kb1 - sh.u0, last = first + pc.KB - 1;
+                const int w0 = (int)(((first + 1) * G - 1) / R), w1 = (int)(((last + 1) * G - 1) / R);
                 __syncwarp();
                 uint32_t old = 0;
-                if (lane == 0) { __threadfence(); old = count_in(p.counters + c0 * 4 + warp); __threadfence(); }
+                if (lane == 0) { __threadfence(); old = count_in(p.counters + (w0 * CG + rank) * FP_EPI_WARPS + warp); __threadfence(); }
                 old = __shfl_sync(0xFFFFFFFFu, old, 0);
-                finish = (int)old == c1 - c0;
-            }
-            if (finish) {
-                for (int c = 0; c < pc.rows; c += 32) {
-                    float f[32];
-                    if (whole) {
-                        uint32_t v[32];
-                        tmem_ld32(acc + c, v);
-                        tmem_ld_wait();
+                if ((int)old == w1 - w0) {
+#pragma unroll 1
+                    for (int k = 0; k < 2 * CG; ++k) {
+                        const int c = (k >> 1) * 128 + half * 64 + (k & 1) * 32, cols = pc.rows - c;
+                        if (cols <= 0) continue;
+                        uint32_t f[32];
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(v[i]);
-                    } else {
+                        for (int i = 0; i < 32; ++i) f[i] = 0;
+                        // two workers' sums on their way at a time, added in the workers' order
+                        for (int q = w0; q <= w1; q += 2) {
+                            const uint4* from = slot_of(q, q == w0) + (c >> 3) * 256;
+                            const uint4* from1 = slot_of(min(q + 1, w1), false) + (c >> 3) * 256;
+                            uint4 a[8], b[8];
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) f[i] = 0.f;
-                        for (int q = c0; q <= c1; ++q) {
-                            const float* slot = p.partials + ((size_t)q * 2 + (q == c0 ? 1 : 0)) * p.TN * 128 + warp * 32 + lane;
+                            for (int i = 0; i < 8; ++i) {
+                                a[i] = b[i] = make_uint4(0, 0, 0, 0);
+                                if (8 * (i >> 1) < cols) { a[i] = __ldcg(from + i * 128); if (q < w1) b[i] = __ldcg(from1 + i * 128); }
+                            }
 #pragma unroll
-                            for (int i = 0; i < 32; ++i)
-                                if (c + i < pc.rows) f[i] += __ldcg(slot + (c + i) * 128);
+                            for (int i = 0; i < 8; ++i) {
+                                const int r = 16 * (i & 1) + 4 * (i >> 1);
+                                const uint32_t x[4] = {a[i].x, a[i].y, a[i].z, a[i].w}, y[4] = {b[i].x, b[i].y, b[i].z, b[i].w};
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) f[r + k] = __float_as_uint(__uint_as_float(f[r + k]) + __uint_as_float(x[k]) + __uint_as_float(y[k]));
+                            }
                         }
-                    }
-                    const int cols = pc.rows - c;
-                    const int to = lane < cols ? p.perm[j0 + c + lane] : 0;
-                    if (ow) {
-                        const float x = lane < cols ? ox[c + lane] : 0.f;
+                        int t = to[0][0];
+                        float x = sx[0][0];
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) f[i] *= w * __shfl_sync(0xFFFFFFFFu, x, i);
+                        for (int i = 1; i < 2 * CG; ++i)
+                            if (i == k) { t = to[i >> 1][i & 1]; x = sx[i >> 1][i & 1]; }
+                        pack_block(f, ow != nullptr, w, x, lane, o);
+                        store_block(p, o, box, t, cols, n0, lane);
                     }
-                    store_columns(p, f, to, cols, n, lane);
                 }
             }
-            tc_fence_before();
-            mbar_arrive(bar_accempty + 8 * buf);
             ++uses;
         }
     }
@@ -373,14 +629,25 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
         while (global_ns() - t0 < 200000ull) __nanosleep(1000);
         __syncthreads();
     }
-    if (warp == 5) {
+    if constexpr (CG == 2) cluster_sync();                 // (the other CTA's copies, MMAs and arrivals are done too)
+    if (warp == FP_MMA_WARP) {
         __syncwarp();
         tc_fence_after();
-        tmem_dealloc(tmem, 512);
+        fp_tmem_dealloc<CG>(tmem);
     }
 }
 
-int tile_tokens(int M) { return M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128; }
+// Tokens of a tile, and whether two SMs share it.
+struct FpTile { int TN; bool pair; };
+FpTile pick_tile(int M, int NT) {
+    if (M <= 64) return {M <= 16 ? 16 : M <= 32 ? 32 : 64, false};
+    const long long workers = device_sm_count();
+    if (M > 128 && 4ll * ((NT + 1) / 2) * ((M + 255) / 256) >= workers) return {256, true};
+    return {M <= 128 || 2ll * NT * ((M + 127) / 128) >= workers ? 128 : 64, false};
+}
+
+// rows of a block of scales: a tile's scales begin at a block's
+int fp_sf_shift(int M, int NT) { return M > 64 && pick_tile(M, NT).TN == 64 ? 6 : 7; }
 
 size_t al256(size_t x) { return (x + 255) / 256 * 256; }
 
@@ -401,7 +668,7 @@ FpLayout fp_layout(int M, const moqe_fp_expert* const* ex, int E) {
     w.sort = off;     off += al256(sort_workspace_bytes(M, E));
     w.counters = off; off += al256((size_t)fp_gemm_counters() * 4);
     w.codes = off;    off += al256(blocks * 128 * w.row_bytes);
-    w.sf = off;       off += al256(blocks * w.block_sf);
+    w.sf = off;       off += al256((blocks << (7 - fp_sf_shift(M, ex[0]->Np / 128))) * w.block_sf);
     w.outer = off;    off += al256(blocks * 128 * 4);
     w.partials = off; off += al256(fp_gemm_partial_bytes(M));
     w.total = off;
@@ -427,7 +694,7 @@ moqe_status fp_args(const void* X, const void* rows, const void* offsets, int M,
 
 moqe_status fp_run(const void* X, const int32_t* perm, const int32_t* offsets, int M, const moqe_fp_expert* const* ex, int E, void* Y,
                    char* base, const FpLayout& w, cudaStream_t st) {
-    FpTokens t = {(uint8_t*)base + w.codes, (uint8_t*)base + w.sf, (float*)(base + w.outer), w.row_bytes, w.block_sf};
+    FpTokens t = {(uint8_t*)base + w.codes, (uint8_t*)base + w.sf, (float*)(base + w.outer), w.row_bytes, w.block_sf, fp_sf_shift(M, ex[0]->Np / 128)};
     FpExperts formats;
     for (int e = 0; e < E; ++e) formats.format[e] = (uint8_t)ex[e]->format;
     uint32_t* counters = (uint32_t*)(base + w.counters);
@@ -438,8 +705,8 @@ moqe_status fp_run(const void* X, const int32_t* perm, const int32_t* offsets, i
 
 }  // namespace
 
-int fp_gemm_counters() { return device_sm_count() * 4; }
-size_t fp_gemm_partial_bytes(int M) { return (size_t)device_sm_count() * 2 * tile_tokens(M) * 128 * 4; }
+int fp_gemm_counters() { return device_sm_count() * FP_EPI_WARPS; }
+size_t fp_gemm_partial_bytes(int M) { return (size_t)device_sm_count() * 2 * (M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : M <= 128 ? 128 : 256) * 128 * 4; }
 
 moqe_status launch_fp_gemm(const moqe_fp_expert* const* ex, int E, int M, const int32_t* perm, const int32_t* offsets, const FpTokens& tokens,
                            uint32_t* counters, void* partials, void* Y, cudaStream_t st) {
@@ -450,25 +717,36 @@ moqe_status launch_fp_gemm(const moqe_fp_expert* const* ex, int E, int M, const 
         const int b = fp_sf_bytes(ex[e]->format);
         sf = b > sf ? b : sf;
     }
-    p.perm = perm; p.offsets = offsets; p.t = tokens; p.counters = counters; p.partials = (float*)partials; p.Y = (__nv_bfloat16*)Y;
+    p.perm = perm; p.offsets = offsets; p.t = tokens; p.counters = counters; p.partials = (uint4*)partials; p.Y = (__nv_bfloat16*)Y;
     p.status = device_status_word();
     if (!p.status) return MOQE_ERR_ALLOC;
-    p.E = E; p.N = ex[0]->N; p.NT = ex[0]->Np / 128; p.TN = tile_tokens(M);
+    p.E = E; p.N = ex[0]->N; p.NT = ex[0]->Np / 128;
+    const FpTile tile = pick_tile(M, p.NT);
+    const bool pair = tile.pair;
+    p.TN = tile.TN;
     // a stage: weights, their scales, token rows (from a multiple of 1024), their scales
     p.b_off = 16384 + sf;
-    p.sfb_off = p.b_off + p.TN * 128;
-    p.stage_bytes = (p.sfb_off + sf + 1023) & ~1023;
+    p.sfb_off = p.b_off + (pair ? p.TN / 2 : p.TN) * 128;
+    p.stage_bytes = (p.sfb_off + (pair ? 2 * sf : sf) + 1023) & ~1023;
     p.stages = FP_RING_BYTES / p.stage_bytes;
     if (p.stages > FP_MAX_STAGES) p.stages = FP_MAX_STAGES;
-    static std::atomic<unsigned long long> attr{0};
-    if (!ensure_dynamic_smem((const void*)fp_gemm_kernel, FP_SMEM, attr)) { cudaGetLastError(); return MOQE_ERR_CUDA; }
+    // (one SM, NVFP4: eight sets of 32 columns behind two accumulators of 128)
+    if (!pair && p.stages > 8) p.stages = 8;
+    static_assert(FP_RING_BYTES / (16384 + 1024 + 16384 + 2048) <= 5, "a pair has room for five sets of 24 columns");
+    p.split_cost = pair ? 18 : 6;
+    p.least_share = pair ? 16 : 4;
+    static std::atomic<unsigned long long> attr[2] = {};
+    const auto kernel = pair ? fp_gemm_kernel<2> : fp_gemm_kernel<1>;
+    if (!ensure_dynamic_smem((const void*)kernel, FP_SMEM, attr[pair])) { cudaGetLastError(); return MOQE_ERR_CUDA; }
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(device_sm_count()); cfg.blockDim = dim3(FP_THREADS); cfg.dynamicSmemBytes = FP_SMEM; cfg.stream = st;
-    cudaLaunchAttribute at[1];
+    cfg.gridDim = dim3(pair ? device_sm_count() & ~1 : device_sm_count()); cfg.blockDim = dim3(FP_THREADS); cfg.dynamicSmemBytes = FP_SMEM; cfg.stream = st;
+    cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = at; cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, fp_gemm_kernel, p) != cudaSuccess) { cudaGetLastError(); return MOQE_ERR_CUDA; }
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = 2; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
+    cfg.attrs = at; cfg.numAttrs = pair ? 2 : 1;
+    if (cudaLaunchKernelEx(&cfg, kernel, p) != cudaSuccess) { cudaGetLastError(); return MOQE_ERR_CUDA; }
     count_launch();
     return MOQE_OK;
 }

@@ -114,7 +114,7 @@ __global__ void fp_tokens_kernel(const __grid_constant__ TokenParams p) {
     const int format = p.formats.format[e];
     const __nv_bfloat16* row = p.X + (size_t)p.perm[j] * p.K;
     const int KB = fp_kblocks(p.K, format);
-    const PackedRow out = token_row(p.t.codes + pad0 * p.t.row_bytes, p.t.sf + (pad0 >> 7) * p.t.block_sf, KB, format, i, seg);
+    const PackedRow out = token_row(p.t.codes + pad0 * p.t.row_bytes, p.t.sf + (pad0 >> p.t.sf_shift) * p.t.block_sf, format, i, seg, p.t.sf_shift);
     if (format == MOQE_FP_MXFP4) pack_row<MOQE_FP_MXFP4>(row, p.K, out, nullptr, buf);
     else if (format == MOQE_FP_NVFP4) pack_row<MOQE_FP_NVFP4>(row, p.K, out, p.t.outer + pad0 + i, buf);
     else {
