@@ -1,5 +1,5 @@
-// Floating-point experts: built from fp32 weights, imported from and exported to canonical arrays.  One block a channel; a thread
-// takes 16 consecutive k at a time.
+// Floating-point experts: built from fp32 weights, imported from and exported to canonical arrays.  One block a channel (see
+// encode_row).
 #include <new>
 
 #include "fp_formats.cuh"
@@ -7,53 +7,26 @@
 namespace moqe {
 namespace {
 
-__device__ __forceinline__ uint4 bf16_x8(const float* x) {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const __nv_bfloat162 v = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-        w[i] = *reinterpret_cast<const uint32_t*>(&v);
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
-}
-
 template <int FORMAT>
-__global__ void fp_build_kernel(const float* __restrict__ W, int N, int K, int KB, uint8_t* tiles, float* outer) {
+__global__ void fp_build_kernel(const float* __restrict__ W, int N, int K, int KB, bool wide, uint8_t* tiles, float* outer) {
     __shared__ uint32_t buf[32];
     const int n = blockIdx.x, padded = KB * fp_kbk(FORMAT);
     const PackedRow out = expert_row(tiles, KB, FORMAT, n);
     const float* row = W + (size_t)n * K;
     const int have = n < N ? K : 0;                         // channels behind the last are zeros
-    int field = 127;
-    if constexpr (FORMAT == MOQE_FP_NVFP4) {
-        uint32_t m = 0;
-        for (int k = threadIdx.x * 16; k < have; k += blockDim.x * 16) {
+    if constexpr (FORMAT == MOQE_FP_BF16) {
+        for (int k = threadIdx.x * 16; k < padded; k += blockDim.x * 16) {
+            RawF32 raw;
+            load16(row, k, have, wide, raw);
             float x[16];
-            load16(row, k, have, x);
-            m = max(m, finite_amax16(x));
+            widen(raw, x);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                *reinterpret_cast<uint4*>(out.chunk(k >> 6, ((k >> 3) & 7) + h)) =
+                    make_uint4(pack_bf16x2(x[8 * h], x[8 * h + 1]), pack_bf16x2(x[8 * h + 2], x[8 * h + 3]), pack_bf16x2(x[8 * h + 4], x[8 * h + 5]), pack_bf16x2(x[8 * h + 6], x[8 * h + 7]));
         }
-        field = nv_row_field(block_max(m, buf));
-        if (threadIdx.x == 0) outer[n] = pow2_field(field);
-    }
-    for (int k0 = 0; k0 < padded; k0 += blockDim.x * 16) {
-        const int k = k0 + threadIdx.x * 16;
-        float x[16];
-        load16(row, k, have, x);
-        if constexpr (FORMAT == MOQE_FP_BF16) {
-            if (k >= padded) continue;
-            const int kb = k >> 6, c = (k >> 3) & 7;
-            *reinterpret_cast<uint4*>(out.chunk(kb, c)) = bf16_x8(x);
-            *reinterpret_cast<uint4*>(out.chunk(kb, c + 1)) = bf16_x8(x + 8);
-        } else {
-            uint32_t a = amax16(x), c[2];
-            if constexpr (FORMAT == MOQE_FP_MXFP4) a = max(a, __shfl_xor_sync(0xFFFFFFFFu, a, 1));
-            const uint32_t byte = encode16<FORMAT, true>(x, a, field, c);
-            if (k >= padded) continue;
-            const int kb = k >> 8, u = (k >> 4) & 15;
-            *reinterpret_cast<uint2*>(out.chunk(kb, u >> 1) + 8 * (u & 1)) = make_uint2(c[0], c[1]);
-            if (FORMAT == MOQE_FP_NVFP4) *out.scale(kb, u) = (uint8_t)byte;
-            else if (!(u & 1)) *out.scale(kb, u >> 1) = (uint8_t)byte;
-        }
+    } else {
+        encode_row<FORMAT>(row, have, padded, wide, buf, outer ? outer + n : nullptr, [&](int k, uint32_t byte, const uint32_t (&c)[2], int) { put_packed<FORMAT>(out, k, padded, byte, c); });
     }
 }
 
@@ -80,9 +53,9 @@ __global__ void fp_import_kernel(const uint8_t* __restrict__ codes, const uint8_
     }
 }
 
-// packed -> canonical arrays
+// packed -> canonical arrays; a thread takes 16 consecutive k at a time.  `wide`: their rows lie on 8-byte (codes) and 32-byte boundaries
 template <int FORMAT>
-__global__ void fp_export_kernel(uint8_t* tiles, const float* outer, int K, int KB, uint8_t* codes, uint8_t* scales, float* outer_out,
+__global__ void fp_export_kernel(uint8_t* tiles, const float* outer, int K, int KB, bool wide, uint8_t* codes, uint8_t* scales, float* outer_out,
                                  __nv_bfloat16* values) {
     const int n = blockIdx.x;
     const PackedRow in = expert_row(tiles, KB, FORMAT, n);
@@ -91,23 +64,33 @@ __global__ void fp_export_kernel(uint8_t* tiles, const float* outer, int K, int 
         o = outer[n];
         if (outer_out && threadIdx.x == 0) outer_out[n] = o;
     }
-    const int size = fp_block(FORMAT), blocks = (K + size - 1) / size;
-    for (int k = threadIdx.x * 8; k < K; k += blockDim.x * 8) {
+    const int blocks = (K + fp_block(FORMAT) - 1) / fp_block(FORMAT);
+    for (int k = threadIdx.x * 16; k < K; k += blockDim.x * 16) {
+        Raw32 r;
         if constexpr (FORMAT == MOQE_FP_BF16) {
-            if (values) *reinterpret_cast<uint4*>(values + (size_t)n * K + k) = *reinterpret_cast<const uint4*>(in.chunk(k >> 6, (k >> 3) & 7));
+            const uint4 a = *reinterpret_cast<const uint4*>(in.chunk(k >> 6, (k >> 3) & 7)), b = *reinterpret_cast<const uint4*>(in.chunk(k >> 6, ((k >> 3) & 7) + 1));
+            r.w[0] = a.x; r.w[1] = a.y; r.w[2] = a.z; r.w[3] = a.w; r.w[4] = b.x; r.w[5] = b.y; r.w[6] = b.z; r.w[7] = b.w;
         } else {
-            const uint32_t c = *reinterpret_cast<const uint32_t*>(in.chunk(k >> 8, (k >> 5) & 7) + ((k >> 1) & 15));
-            const uint32_t byte = *in.scale(k >> 8, (k & 255) / size);
-            if (codes) *reinterpret_cast<uint32_t*>(codes + (size_t)n * (K / 2) + k / 2) = c;
-            if (scales && k % size == 0) scales[(size_t)n * blocks + k / size] = (uint8_t)byte;
-            if (values) {
-                const float s = FORMAT == MOQE_FP_MXFP4 ? e8m0_value(byte) : e4m3_value(byte);
-                float v[8];
+            const uint2 c = *reinterpret_cast<const uint2*>(in.chunk(k >> 8, (k >> 5) & 7) + ((k >> 1) & 8));
+            const uint32_t byte = *in.scale(k >> 8, (k & 255) / fp_block(FORMAT));
+            if (codes) {
+                uint32_t* to = reinterpret_cast<uint32_t*>(codes + (size_t)n * (K / 2) + k / 2);
+                if (wide) *reinterpret_cast<uint2*>(to) = c;
+                else { to[0] = c.x; if (k + 8 < K) to[1] = c.y; }
+            }
+            if (scales && k % fp_block(FORMAT) == 0) scales[(size_t)n * blocks + k / fp_block(FORMAT)] = (uint8_t)byte;
+            if (!values) continue;
+            const float s = FORMAT == MOQE_FP_MXFP4 ? e8m0_value(byte) : e4m3_value(byte);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = e2m1_value((c >> (4 * i)) & 15u) * s * o;
-                *reinterpret_cast<uint4*>(values + (size_t)n * K + k) = bf16_x8(v);
+            for (int h = 0; h < 2; ++h) {
+                float v[8];
+                e2m1_values(h ? c.y : c.x, v);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    r.w[4 * h + i] = FORMAT == MOQE_FP_MXFP4 ? pack_bf16x2(v[2 * i] * s, v[2 * i + 1] * s) : pack_bf16x2(v[2 * i] * s * o, v[2 * i + 1] * s * o);
             }
         }
+        if (values) store32(values + (size_t)n * K + k, (K - k) * 2, wide, r);
     }
 }
 
@@ -149,7 +132,7 @@ extern "C" moqe_status moqe_fp_quantize(const float* W, int N, int K, int format
     moqe_fp_expert* e = nullptr;
     if ((s = fp_alloc(N, K, format, st, &e)) != MOQE_OK) return s;
     const auto kernel = format == MOQE_FP_MXFP4 ? fp_build_kernel<MOQE_FP_MXFP4> : format == MOQE_FP_NVFP4 ? fp_build_kernel<MOQE_FP_NVFP4> : fp_build_kernel<MOQE_FP_BF16>;
-    kernel<<<e->Np, channel_threads(K, 16), 0, st>>>(W, N, K, e->KB, e->tiles, e->outer);
+    kernel<<<e->Np, row_threads(K), 0, st>>>(W, N, K, e->KB, (uintptr_t)W % 32 == 0, e->tiles, e->outer);
     count_launch();
     if (cudaGetLastError() != cudaSuccess) { moqe_fp_expert_destroy(e); return MOQE_ERR_CUDA; }
     *out = e;
@@ -181,7 +164,8 @@ extern "C" moqe_status moqe_fp_expert_export(const moqe_fp_expert* e, uint8_t* c
     if (!codes && !scales && !outer && !values_bf16) return MOQE_OK;
     cudaStream_t st = (cudaStream_t)stream;
     const auto kernel = e->format == MOQE_FP_MXFP4 ? fp_export_kernel<MOQE_FP_MXFP4> : e->format == MOQE_FP_NVFP4 ? fp_export_kernel<MOQE_FP_NVFP4> : fp_export_kernel<MOQE_FP_BF16>;
-    kernel<<<e->N, channel_threads(e->K, 8), 0, st>>>(e->tiles, e->outer, e->K, e->KB, codes, scales, outer, (__nv_bfloat16*)values_bf16);
+    const bool wide = e->K % 16 == 0 && (uintptr_t)codes % 8 == 0 && (uintptr_t)values_bf16 % 32 == 0;
+    kernel<<<e->N, channel_threads(e->K, 16), 0, st>>>(e->tiles, e->outer, e->K, e->KB, wide, codes, scales, outer, (__nv_bfloat16*)values_bf16);
     count_launch();
     return cuda_ok(cudaGetLastError());
 }

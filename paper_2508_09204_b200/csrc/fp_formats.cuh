@@ -77,11 +77,21 @@ __device__ __forceinline__ uint32_t e2m1_x8(const float* v) {
         : "=r"(d) : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
     return d;
 }
-// what a code stands for
-__device__ __forceinline__ float e2m1_value(uint32_t c) {
-    const uint32_t m = c & 7u, sign = (c & 8u) << 28;
-    const uint32_t mag = m < 2 ? m * 0x3F000000u : ((m & 1u) << 22) + ((126u + (m >> 1)) << 23);
-    return __uint_as_float(mag | sign);
+// what eight codes stand for
+__device__ __forceinline__ void e2m1_values(uint32_t codes, float (&v)[8]) {
+    uint32_t h[4];
+    asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\tcvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(codes));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
+        v[2 * i] = f.x; v[2 * i + 1] = f.y;
+    }
+}
+__device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
 }
 // nearest e4m3 number's byte, 0 <= v <= 448
 __device__ __forceinline__ uint32_t e4m3_byte(float v) {
@@ -90,8 +100,9 @@ __device__ __forceinline__ uint32_t e4m3_byte(float v) {
     return d & 0xFFu;
 }
 
-// y / s for y >= 0 and an e4m3 number s > 0 with 1 / s correctly rounded in rs: the correctly rounded quotient (Markstein), moved
-// off a border by a unit of the last place where it is not there exactly (fp32 sources).
+// y / s, rounded to nearest, for s > 0 with 1 / s to an unit or two of the last place in rs (one step of Markstein's correction: where
+// the quotient has few bits, as on a border, it is exact).  fp32 sources: moved off a border by a unit of the last place where it
+// is not there exactly, as the remainder's sign says.
 template <bool FP32>
 __device__ __forceinline__ float nv_quotient(float y, float s, float rs) {
     const float q0 = y * rs;
@@ -103,27 +114,29 @@ __device__ __forceinline__ float nv_quotient(float y, float s, float rs) {
     }
     return q;
 }
+__device__ __forceinline__ float rcp_approx(float s) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s)); return r; }
 
-// Scale and codes of 16 consecutive k of a row.  `amax`: bits of the largest magnitude of the numbers that share the scale;
-// `row_field`: NVFP4's row scale is 2^(row_field - 127).  -> the scale's byte; codes, eight to a word.
+// Scale and codes of 16 consecutive k of a row.  `amax`: the largest magnitude of the numbers that share the scale (a NaN if there is
+// one among them); `row_field`: NVFP4's row scale is 2^(row_field - 127).  -> the scale's byte; the codes, the first in the lowest nibble.
 template <int FORMAT, bool FP32>
-__device__ __forceinline__ uint32_t encode16(const float (&x)[16], uint32_t amax, int row_field, uint32_t (&codes)[2]) {
-    if (amax >= 0x7F800000u) {                              // an infinity or a NaN: the block is a NaN
+__device__ __forceinline__ uint32_t encode16(const float (&x)[16], float amax, int row_field, uint32_t (&codes)[2]) {
+    const uint32_t top = __float_as_uint(amax);
+    if (top >= 0x7F800000u) {                               // an infinity or a NaN: the block is a NaN
         codes[0] = codes[1] = 0;
         return FORMAT == MOQE_FP_MXFP4 ? 255u : 127u;
     }
     float q[16];
     uint32_t byte;
     if constexpr (FORMAT == MOQE_FP_MXFP4) {
-        byte = (uint32_t)max((int)(amax >> 23) - 2, 0);
+        byte = (uint32_t)max((int)(top >> 23) - 2, 0);
         const float inv = pow2_field(254 - (int)byte);
 #pragma unroll
         for (int i = 0; i < 16; ++i) q[i] = x[i] * inv;
     } else {
         const float inv = pow2_field(254 - row_field);
-        byte = e4m3_byte(__fdiv_rn(__uint_as_float(amax) * inv, 6.0f));
+        byte = e4m3_byte(nv_quotient<false>(amax * inv, 6.0f, 1.0f / 6.0f));
         const float s = e4m3_value(byte);
-        const float rs = byte ? __frcp_rn(s) : 0.f;
+        const float rs = byte ? rcp_approx(s) : 0.f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) q[i] = copysignf(nv_quotient<FP32>(fabsf(x[i]) * inv, s, rs), x[i]);
     }
@@ -134,39 +147,62 @@ __device__ __forceinline__ uint32_t encode16(const float (&x)[16], uint32_t amax
 // NVFP4: the row scale's exponent field for the bits of the row's largest finite magnitude
 __device__ __forceinline__ int nv_row_field(uint32_t amax) { return amax == 0 ? 127 : max((int)(amax >> 23) - 10, 1); }
 
-// 16 consecutive k of a row, zeros behind its end (K is a multiple of 8)
-__device__ __forceinline__ void load16(const __nv_bfloat16* row, int k, int K, float (&x)[16]) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const uint4 v = k + 8 * h < K ? *reinterpret_cast<const uint4*>(row + k + 8 * h) : make_uint4(0, 0, 0, 0);
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[8 * h + 2 * i] = __uint_as_float(w[i] << 16);
-            x[8 * h + 2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-        }
+// Rows are taken in chunks of 16 consecutive k, neighbouring lanes neighbouring chunks; two lanes agree on a scale of MXFP4.  (With
+// eight to a chunk the shared work of a block, its scale and the addresses, made 16384 x 11008 take 161 instead of 130 us.)  A thread
+// holds ROW_CHUNKS of them, all loaded before the first is used.
+constexpr int ROW_CHUNKS = 2;
+struct Raw32 { uint32_t w[8]; };
+// 32 bytes, of which `have` (0, 16 or all) are read; `wide`: from a 32-byte boundary
+__device__ __forceinline__ void load32(const void* p, int have, bool wide, Raw32& r) {
+    if (wide && have >= 32) {
+        asm volatile("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]), "=r"(r.w[4]), "=r"(r.w[5]), "=r"(r.w[6]), "=r"(r.w[7]) : "l"(p));
+        return;
     }
+    const uint4 z = make_uint4(0, 0, 0, 0), *q = reinterpret_cast<const uint4*>(p);
+    const uint4 a = have > 0 ? __ldg(q) : z, b = have > 16 ? __ldg(q + 1) : z;
+    r.w[0] = a.x; r.w[1] = a.y; r.w[2] = a.z; r.w[3] = a.w; r.w[4] = b.x; r.w[5] = b.y; r.w[6] = b.z; r.w[7] = b.w;
 }
-__device__ __forceinline__ void load16(const float* row, int k, int K, float (&x)[16]) {
-#pragma unroll
-    for (int h = 0; h < 4; ++h) {
-        const float4 v = k + 4 * h < K ? *reinterpret_cast<const float4*>(row + k + 4 * h) : make_float4(0.f, 0.f, 0.f, 0.f);
-        x[4 * h] = v.x; x[4 * h + 1] = v.y; x[4 * h + 2] = v.z; x[4 * h + 3] = v.w;
+__device__ __forceinline__ void store32(void* p, int have, bool wide, const Raw32& r) {
+    if (wide && have >= 32) {
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                     ::"l"(p), "r"(r.w[0]), "r"(r.w[1]), "r"(r.w[2]), "r"(r.w[3]), "r"(r.w[4]), "r"(r.w[5]), "r"(r.w[6]), "r"(r.w[7]) : "memory");
+        return;
     }
+    uint4* q = reinterpret_cast<uint4*>(p);
+    if (have > 0) q[0] = make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
+    if (have > 16) q[1] = make_uint4(r.w[4], r.w[5], r.w[6], r.w[7]);
 }
-__device__ __forceinline__ uint32_t magnitude_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
-__device__ __forceinline__ uint32_t amax16(const float (&x)[16]) {
-    uint32_t m = 0;
+// 16 numbers of a row, zeros behind its end (K is a multiple of 8)
+struct RawBf16 { Raw32 r; };
+struct RawF32 { Raw32 a, b; };
+__device__ __forceinline__ void load16(const __nv_bfloat16* row, int k, int K, bool wide, RawBf16& raw) { load32(row + k, (K - k) * 2, wide, raw.r); }
+__device__ __forceinline__ void load16(const float* row, int k, int K, bool wide, RawF32& raw) {
+    load32(row + k, (K - k) * 4, wide, raw.a);
+    load32(row + k + 8, (K - k - 8) * 4, wide, raw.b);
+}
+__device__ __forceinline__ void widen(const RawBf16& raw, float (&x)[16]) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) m = max(m, magnitude_bits(x[i]));
-    return m;
+    for (int i = 0; i < 8; ++i) { x[2 * i] = __uint_as_float(raw.r.w[i] << 16); x[2 * i + 1] = __uint_as_float(raw.r.w[i] & 0xFFFF0000u); }
+}
+__device__ __forceinline__ void widen(const RawF32& raw, float (&x)[16]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { x[i] = __uint_as_float(raw.a.w[i]); x[8 + i] = __uint_as_float(raw.b.w[i]); }
+}
+// the largest magnitude; a NaN if there is one
+__device__ __forceinline__ float max_abs3(float a, float b, float c) { float d; asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c)); return d; }
+__device__ __forceinline__ float amax16(const float (&x)[16]) {
+    float m = max_abs3(x[0], x[1], x[2]);
+#pragma unroll
+    for (int i = 3; i < 15; i += 2) m = max_abs3(m, x[i], x[i + 1]);
+    return max_abs3(m, x[15], x[15]);
 }
 __device__ __forceinline__ uint32_t finite_amax16(const float (&x)[16]) {
-    uint32_t m = amax16(x);
+    uint32_t m = __float_as_uint(amax16(x));
     if (m >= 0x7F800000u) {
         m = 0;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) { const uint32_t b = magnitude_bits(x[i]); m = max(m, b < 0x7F800000u ? b : 0u); }
+        for (int i = 0; i < 16; ++i) { const uint32_t b = __float_as_uint(x[i]) & 0x7FFFFFFFu; m = max(m, b < 0x7F800000u ? b : 0u); }
     }
     return m;
 }
@@ -177,6 +213,66 @@ __device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t* buf) {
     __syncthreads();
     v = threadIdx.x % 32 < blockDim.x / 32 ? buf[threadIdx.x & 31] : 0u;
     return __reduce_max_sync(0xFFFFFFFFu, v);
+}
+
+// One row by the whole block: every chunk of the `padded` k is encoded and handed to `sink(k, byte, codes, field)` by all lanes of its
+// warp together; NVFP4's row scale comes first (from registers where the row fits into them, else the row is read twice).
+// `wide`: rows begin on 32-byte boundaries.
+template <class T> struct RawOf { typedef RawBf16 type; };
+template <> struct RawOf<float> { typedef RawF32 type; };
+template <int FORMAT, class T, class Sink>
+__device__ __forceinline__ void encode_row(const T* row, int have, int padded, bool wide, uint32_t* buf, float* outer, Sink sink) {
+    constexpr bool FP32 = sizeof(T) == 4;
+    const int span = blockDim.x * 16 * ROW_CHUNKS, parts = (padded + span - 1) / span, k0 = threadIdx.x * 16, step = blockDim.x * 16;
+    typename RawOf<T>::type raw[ROW_CHUNKS];
+    int field = 127;
+    if constexpr (FORMAT == MOQE_FP_NVFP4) {
+        uint32_t m = 0;
+        for (int part = 0; part < parts; ++part) {
+#pragma unroll
+            for (int i = 0; i < ROW_CHUNKS; ++i) load16(row, part * span + k0 + i * step, have, wide, raw[i]);
+#pragma unroll
+            for (int i = 0; i < ROW_CHUNKS; ++i) { float x[16]; widen(raw[i], x); m = max(m, finite_amax16(x)); }
+        }
+        field = nv_row_field(block_max(m, buf));
+        if (outer && threadIdx.x == 0) *outer = pow2_field(field);
+    }
+    for (int part = 0; part < parts; ++part) {
+        if (FORMAT != MOQE_FP_NVFP4 || parts > 1) {
+#pragma unroll
+            for (int i = 0; i < ROW_CHUNKS; ++i) load16(row, part * span + k0 + i * step, have, wide, raw[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < ROW_CHUNKS; ++i) {
+            const int k = part * span + k0 + i * step;
+            if (k - (int)(threadIdx.x & 31) * 16 >= padded) break;         // (the whole warp)
+            float x[16];
+            widen(raw[i], x);
+            float a = amax16(x);
+            uint32_t codes[2];
+            if constexpr (FORMAT == MOQE_FP_MXFP4) { const float b = __shfl_xor_sync(0xFFFFFFFFu, a, 1); a = max_abs3(a, b, b); }
+            const uint32_t byte = encode16<FORMAT, FP32>(x, a, field, codes);
+            sink(k, byte, codes, field);
+        }
+    }
+}
+// Threads of a block that takes a row, so that the row fits into their registers if it can.
+inline int row_threads(int K) {
+    const int t = ((K + 15) / 16 + ROW_CHUNKS - 1) / ROW_CHUNKS;
+    return t >= 512 ? 512 : (t + 31) / 32 * 32;
+}
+// ... into a packed row: four scales to a store.  (All lanes of a warp; `padded` is a multiple of 256, so half warps are there as a whole.)
+template <int FORMAT>
+__device__ __forceinline__ void put_packed(const PackedRow& out, int k, int padded, uint32_t byte, const uint32_t (&codes)[2]) {
+    constexpr int LANES = FORMAT == MOQE_FP_MXFP4 ? 2 : 1;                 // of a block
+    const int kb = k >> 8, in = k & 255;
+    uint32_t w = byte;
+    w |= __shfl_down_sync(0xFFFFFFFFu, byte, LANES) << 8;
+    w |= __shfl_down_sync(0xFFFFFFFFu, byte, 2 * LANES) << 16;
+    w |= __shfl_down_sync(0xFFFFFFFFu, byte, 3 * LANES) << 24;
+    if (k >= padded) return;
+    *reinterpret_cast<uint2*>(out.chunk(kb, in >> 5) + ((in >> 1) & 8)) = make_uint2(codes[0], codes[1]);
+    if ((threadIdx.x & (4 * LANES - 1)) == 0) *reinterpret_cast<uint32_t*>(out.scale(kb, in / (16 * LANES))) = w;
 }
 
 // quantize.cu: device memory of experts (a pool of the library's)
