@@ -26,7 +26,7 @@ __global__ void fp_build_kernel(const float* __restrict__ W, int N, int K, int K
                     make_uint4(pack_bf16x2(x[8 * h], x[8 * h + 1]), pack_bf16x2(x[8 * h + 2], x[8 * h + 3]), pack_bf16x2(x[8 * h + 4], x[8 * h + 5]), pack_bf16x2(x[8 * h + 6], x[8 * h + 7]));
         }
     } else {
-        encode_row<FORMAT>(row, have, padded, wide, buf, outer ? outer + n : nullptr, [&](int k, uint32_t byte, const uint32_t (&c)[2], int) { put_packed<FORMAT>(out, k, padded, byte, c); });
+        encode_row<FORMAT, 2>(row, have, padded, wide, buf, outer ? outer + n : nullptr, [&](int k, uint32_t byte, const uint32_t (&c)[2], int) { put_packed<FORMAT>(out, k, padded, byte, c); });
     }
 }
 
@@ -132,7 +132,7 @@ extern "C" moqe_status moqe_fp_quantize(const float* W, int N, int K, int format
     moqe_fp_expert* e = nullptr;
     if ((s = fp_alloc(N, K, format, st, &e)) != MOQE_OK) return s;
     const auto kernel = format == MOQE_FP_MXFP4 ? fp_build_kernel<MOQE_FP_MXFP4> : format == MOQE_FP_NVFP4 ? fp_build_kernel<MOQE_FP_NVFP4> : fp_build_kernel<MOQE_FP_BF16>;
-    kernel<<<e->Np, row_threads(K), 0, st>>>(W, N, K, e->KB, (uintptr_t)W % 32 == 0, e->tiles, e->outer);
+    kernel<<<e->Np, row_threads(K, 2), 0, st>>>(W, N, K, e->KB, (uintptr_t)W % 32 == 0, e->tiles, e->outer);
     count_launch();
     if (cudaGetLastError() != cudaSuccess) { moqe_fp_expert_destroy(e); return MOQE_ERR_CUDA; }
     *out = e;

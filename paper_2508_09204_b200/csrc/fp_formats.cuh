@@ -149,8 +149,8 @@ __device__ __forceinline__ int nv_row_field(uint32_t amax) { return amax == 0 ? 
 
 // Rows are taken in chunks of 16 consecutive k, neighbouring lanes neighbouring chunks; two lanes agree on a scale of MXFP4.  (With
 // eight to a chunk the shared work of a block, its scale and the addresses, made 16384 x 11008 take 161 instead of 130 us.)  A thread
-// holds ROW_CHUNKS of them, all loaded before the first is used.
-constexpr int ROW_CHUNKS = 2;
+// holds CHUNKS of them, all loaded before the first is used: two where rows are few and a row's latency counts, more where there
+// are many, so that what a block does once for a row weighs less.
 struct Raw32 { uint32_t w[8]; };
 // 32 bytes, of which `have` (0, 16 or all) are read; `wide`: from a 32-byte boundary
 __device__ __forceinline__ void load32(const void* p, int have, bool wide, Raw32& r) {
@@ -220,19 +220,19 @@ __device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t* buf) {
 // `wide`: rows begin on 32-byte boundaries.
 template <class T> struct RawOf { typedef RawBf16 type; };
 template <> struct RawOf<float> { typedef RawF32 type; };
-template <int FORMAT, class T, class Sink>
+template <int FORMAT, int CHUNKS, class T, class Sink>
 __device__ __forceinline__ void encode_row(const T* row, int have, int padded, bool wide, uint32_t* buf, float* outer, Sink sink) {
     constexpr bool FP32 = sizeof(T) == 4;
-    const int span = blockDim.x * 16 * ROW_CHUNKS, parts = (padded + span - 1) / span, k0 = threadIdx.x * 16, step = blockDim.x * 16;
-    typename RawOf<T>::type raw[ROW_CHUNKS];
+    const int span = blockDim.x * 16 * CHUNKS, parts = (padded + span - 1) / span, k0 = threadIdx.x * 16, step = blockDim.x * 16;
+    typename RawOf<T>::type raw[CHUNKS];
     int field = 127;
     if constexpr (FORMAT == MOQE_FP_NVFP4) {
         uint32_t m = 0;
         for (int part = 0; part < parts; ++part) {
 #pragma unroll
-            for (int i = 0; i < ROW_CHUNKS; ++i) load16(row, part * span + k0 + i * step, have, wide, raw[i]);
+            for (int i = 0; i < CHUNKS; ++i) load16(row, part * span + k0 + i * step, have, wide, raw[i]);
 #pragma unroll
-            for (int i = 0; i < ROW_CHUNKS; ++i) { float x[16]; widen(raw[i], x); m = max(m, finite_amax16(x)); }
+            for (int i = 0; i < CHUNKS; ++i) { float x[16]; widen(raw[i], x); m = max(m, finite_amax16(x)); }
         }
         field = nv_row_field(block_max(m, buf));
         if (outer && threadIdx.x == 0) *outer = pow2_field(field);
@@ -240,10 +240,10 @@ __device__ __forceinline__ void encode_row(const T* row, int have, int padded, b
     for (int part = 0; part < parts; ++part) {
         if (FORMAT != MOQE_FP_NVFP4 || parts > 1) {
 #pragma unroll
-            for (int i = 0; i < ROW_CHUNKS; ++i) load16(row, part * span + k0 + i * step, have, wide, raw[i]);
+            for (int i = 0; i < CHUNKS; ++i) load16(row, part * span + k0 + i * step, have, wide, raw[i]);
         }
 #pragma unroll
-        for (int i = 0; i < ROW_CHUNKS; ++i) {
+        for (int i = 0; i < CHUNKS; ++i) {
             const int k = part * span + k0 + i * step;
             if (k - (int)(threadIdx.x & 31) * 16 >= padded) break;         // (the whole warp)
             float x[16];
@@ -257,8 +257,8 @@ __device__ __forceinline__ void encode_row(const T* row, int have, int padded, b
     }
 }
 // Threads of a block that takes a row, so that the row fits into their registers if it can.
-inline int row_threads(int K) {
-    const int t = ((K + 15) / 16 + ROW_CHUNKS - 1) / ROW_CHUNKS;
+inline int row_threads(int K, int chunks) {
+    const int t = ((K + 15) / 16 + chunks - 1) / chunks;
     return t >= 512 ? 512 : (t + 31) / 32 * 32;
 }
 // ... into a packed row: four scales to a store.  (All lanes of a warp; `padded` is a multiple of 256, so half warps are there as a whole.)

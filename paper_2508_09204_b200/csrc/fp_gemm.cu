@@ -24,6 +24,7 @@
 namespace moqe {
 namespace {
 
+constexpr int FP_COST_4BIT = 5, FP_COST_BF16 = 4;      // of a k-block (16 rows x 4096 -> 11008, equal costs: bf16 tiles were done after 22, 4-bit ones after 27 us)
 constexpr int FP_BAND = 8;                       // token tiles that are gone through together (see FpWalk)
 constexpr int FP_EPI_WARPS = 8;
 constexpr int FP_WEIGHTS_WARP = FP_EPI_WARPS, FP_MMA_WARP = FP_EPI_WARPS + 1, FP_TOKENS_WARP = FP_EPI_WARPS + 2;
@@ -58,52 +59,76 @@ struct FpGemmParams {
 
 struct FpSched {
     // by place in the order of work: 4-bit experts first, then the bf16 ones, whose tiles are four times as deep
-    int order[MOQE_MAX_EXPERTS], tile0[MOQE_MAX_EXPERTS + 1], unit0[MOQE_MAX_EXPERTS + 1], KB[MOQE_MAX_EXPERTS], tts[MOQE_MAX_EXPERTS];
+    int order[MOQE_MAX_EXPERTS], tile0[MOQE_MAX_EXPERTS + 1], unit0[MOQE_MAX_EXPERTS + 1], KB[MOQE_MAX_EXPERTS], cost[MOQE_MAX_EXPERTS], tts[MOQE_MAX_EXPERTS];
     int off[MOQE_MAX_EXPERTS + 1], pad0[MOQE_MAX_EXPERTS];      // by expert
     int W, NT;                   // workers (CTAs or pairs); channel tiles of a worker
-    int whole, u0, R, G;         // tiles dealt out whole; then R k-blocks from u0 on in equal shares for G workers
+    int whole, u0, G, q, r;      // tiles dealt out whole; then what costs from u0 on in equal shares for G workers: q G + r
     uint32_t tmem;
     int abort;
+    // Where worker w's share begins (u0 and the end of everything for w = 0 and G): a k-block belongs to the share that its start
+    // is in.
+    __device__ __forceinline__ int cut(int w) const { return u0 + w * q + (int)((unsigned)(w * r) / (unsigned)G); }
 };
 
-// k-blocks [kb0, kb1) of channel tile nt of the tokens [i0, i0 + rows) of expert e
-struct FpPiece { int e, nt, i0, rows, kb0, kb1, KB; };
+// k-blocks [kb0, kb1) of channel tile nt of the tokens [i0, i0 + rows) of expert e; at: its place in the order; tile: the expert's
+struct FpPiece { int e, nt, i0, rows, kb0, kb1, KB, at, tile; };
 
-// What one worker does, piece after piece; every role walks it for itself.  Tiles lie in bands of FP_BAND token tiles, in a band
-// channel tile by channel tile, so that the workers of a moment share both token and weight tiles in L2.  Whole tiles go to the
-// workers in turn; the rest are one sequence of k-blocks, cut into equal shares.
+// a / b for 0 <= a, 0 < b (a 32-bit division takes far longer; the quotient is a few units off at most)
+__device__ __forceinline__ int div_small(int a, int b) {
+    int q = (int)((float)a * __frcp_rz((float)b));
+    while ((q + 1) * b <= a) ++q;
+    while (q * b > a) --q;
+    return q;
+}
+// tokens [i0, i0 + rows) and channel tile of an expert's tile: bands of FP_BAND token tiles, in a band channel tile by channel tile
+__device__ __forceinline__ void place_tile(const FpSched& s, int TN, FpPiece& pc) {
+    const int band = div_small(pc.tile, FP_BAND * s.NT), in = pc.tile - band * FP_BAND * s.NT, deep = min(FP_BAND, s.tts[pc.at] - band * FP_BAND);
+    pc.e = s.order[pc.at];
+    pc.nt = div_small(in, deep);
+    pc.i0 = (band * FP_BAND + in - pc.nt * deep) * TN;
+    pc.rows = min(TN, s.off[pc.e + 1] - s.off[pc.e] - pc.i0);
+}
+
+// What one worker does, piece after piece; every role walks it for itself.  Bands of tiles make the workers of a moment share both
+// token and weight tiles in L2.  Whole tiles go to the workers in turn; the rest are one sequence of k-blocks, cut into shares of
+// equal cost (a 4-bit k-block brings scales, and its tiles are short).
 struct FpWalk {
     int at, t, u, ue;
     __device__ __forceinline__ void start(const FpSched& s, int w) {
         at = 0;
         t = w;
         u = ue = 0;
-        if (w < s.G) { u = s.u0 + (int)((long long)w * s.R / s.G); ue = s.u0 + (int)((long long)(w + 1) * s.R / s.G); }
+        if (w < s.G) { u = s.cut(w); ue = s.cut(w + 1); }
     }
     __device__ __forceinline__ bool next(const FpSched& s, const FpGemmParams& p, FpPiece& pc) {
-        int tile;
         if (t < s.whole) {
             while (t >= s.tile0[at + 1]) ++at;
-            tile = t - s.tile0[at];
+            pc.tile = t - s.tile0[at];
             pc.KB = s.KB[at];
             pc.kb0 = 0;
             pc.kb1 = pc.KB;
             t += s.W;
         } else {
-            if (u >= ue) return false;
-            while (u >= s.unit0[at + 1]) ++at;
-            const int v = u - s.unit0[at];
+            // (u, ue: in costs; the k-blocks that begin in [u, ue))
+            int c, v, end;
+            for (;;) {
+                if (u >= ue) return false;
+                while (u >= s.unit0[at + 1]) ++at;
+                const int to = min(ue, s.unit0[at + 1]);
+                c = s.cost[at];
+                v = div_small(u - s.unit0[at] + c - 1, c);
+                end = div_small(to - s.unit0[at] + c - 1, c);
+                if (v < end) break;
+                u = to;
+            }
             pc.KB = s.KB[at];
-            tile = v / pc.KB;
-            pc.kb0 = v - tile * pc.KB;
-            pc.kb1 = min(pc.KB, pc.kb0 + ue - u);
-            u += pc.kb1 - pc.kb0;
+            pc.tile = div_small(v, pc.KB);
+            pc.kb0 = v - pc.tile * pc.KB;
+            pc.kb1 = min(pc.KB, pc.kb0 + end - v);
+            u = s.unit0[at] + (pc.tile * pc.KB + pc.kb1) * c;
         }
-        pc.e = s.order[at];
-        const int band = tile / (FP_BAND * s.NT), in = tile - band * FP_BAND * s.NT, deep = min(FP_BAND, s.tts[at] - band * FP_BAND);
-        pc.nt = in / deep;
-        pc.i0 = (band * FP_BAND + in - pc.nt * deep) * p.TN;
-        pc.rows = min(p.TN, s.off[pc.e + 1] - s.off[pc.e] - pc.i0);
+        pc.at = at;
+        place_tile(s, p.TN, pc);
         return true;
     }
 };
@@ -350,7 +375,7 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
     const uint32_t bar_full = smem_u32(bars), bar_empty = bar_full + 8 * FP_MAX_STAGES;
     const uint32_t bar_accfull = bar_empty + 8 * FP_MAX_STAGES, bar_accempty = bar_accfull + 16;
 
-    if (threadIdx.x == 0) {
+    if (threadIdx.x == FP_WEIGHTS_WARP * 32) {
         // (weights and tokens arrive on their own; a pair's first CTA issues the MMAs: its full barriers take an arrival for the other CTA, too)
         for (int i = 0; i < p.stages; ++i) { mbar_init(bar_full + 8 * i, CG == 2 && rank == 0 ? 3 : 2); mbar_init(bar_empty + 8 * i, 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(bar_accfull + 8 * i, 1); mbar_init(bar_accempty + 8 * i, FP_EPI_WARPS * CG); }
@@ -382,38 +407,49 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
         {
             const bool is = lane < p.E;
             const int e = is ? sh.order[lane] : 0, rows = is ? sh.off[e + 1] - sh.off[e] : 0, KB = is ? p.ex[e].KB : 1, NT = (p.NT + CG - 1) / CG;
-            const int tts = (rows + p.TN - 1) / p.TN, tiles = tts * NT;
-            int tsum = tiles, usum = tiles * KB;
+            const int tts = (rows + p.TN - 1) / p.TN, tiles = tts * NT, cost = is && p.ex[e].format == MOQE_FP_BF16 ? FP_COST_BF16 : FP_COST_4BIT, units = tiles * KB * cost;
+            int tsum = tiles, usum = units;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
                 const int a = __shfl_up_sync(0xFFFFFFFFu, tsum, d), b = __shfl_up_sync(0xFFFFFFFFu, usum, d);
                 if (lane >= d) { tsum += a; usum += b; }
             }
             if (is) {
-                sh.tile0[lane] = tsum - tiles; sh.unit0[lane] = usum - tiles * KB; sh.KB[lane] = KB; sh.tts[lane] = tts;
+                sh.tile0[lane] = tsum - tiles; sh.unit0[lane] = usum - units; sh.KB[lane] = KB; sh.cost[lane] = cost; sh.tts[lane] = tts;
                 if (lane == p.E - 1) { sh.tile0[p.E] = tsum; sh.unit0[p.E] = usum; }
             }
             // Rounds of whole tiles; what does not fill a round, and the round before it, are split if that saves more k-blocks than
             // parking and adding up cost.
             const int T = __shfl_sync(0xFFFFFFFFu, tsum, 31), U = __shfl_sync(0xFFFFFFFFu, usum, 31), W = (int)gridDim.x / CG;
             const uint32_t some = __ballot_sync(0xFFFFFFFFu, tiles > 0);
-            const int left = T % W, KBlast = __shfl_sync(0xFFFFFFFFu, KB, some ? 31 - __clz(some) : 0);
+            const int last = some ? 31 - __clz(some) : 0, deepest = __shfl_sync(0xFFFFFFFFu, KB * cost, last), left = T % W;
+            const bool alike = __all_sync(0xFFFFFFFFu, tiles == 0 || KB * cost == deepest);
             int whole = T;
-            if (left != 0 && (long long)KBlast * (W - left) > (long long)p.split_cost * W) whole = T < W ? 0 : T - left - W;
+            if (left != 0 && (long long)deepest * (W - left) > (long long)p.split_cost * FP_COST_BF16 * W) whole = T < W ? 0 : T - left - W;
             const uint32_t holds = __ballot_sync(0xFFFFFFFFu, is && whole >= tsum - tiles && whole < tsum);
             const int at = holds ? __ffs(holds) - 1 : 0;
-            const int u0 = whole < T ? __shfl_sync(0xFFFFFFFFu, usum - tiles * KB + (whole - (tsum - tiles)) * KB, at) : U;
+            const int u0 = whole < T ? __shfl_sync(0xFFFFFFFFu, usum - units + (whole - (tsum - tiles)) * KB * cost, at) : U;
             if (lane == 0) {
-                sh.W = W; sh.NT = NT; sh.whole = whole; sh.u0 = u0; sh.R = U - u0;
-                sh.G = U > u0 ? max(1, min(W, (U - u0) / p.least_share)) : 0;
+                const int R = U - u0;
+                int G = R > 0 ? max(1, min(W, R / (p.least_share * FP_COST_BF16))) : 0;
+                // few tiles, all alike: the same number of workers for each, so that nobody has the ends of two, if that is not much longer
+                if (alike && whole == 0 && T <= G && deepest / (G / T) <= R / G + p.split_cost * FP_COST_BF16) G = G / T * T;
+                sh.W = W; sh.NT = NT; sh.whole = whole; sh.u0 = u0; sh.G = G;
+                sh.q = G ? R / G : 0; sh.r = G ? R - sh.q * G : 0;
             }
         }
     }
+    // The weights' warp, which has set up all but tensor memory, goes ahead: it has nothing to do with the other CTA.
     tc_fence_before();
-    __syncthreads();
-    if constexpr (CG == 2) cluster_sync();
+    __syncwarp();
+    if (warp == FP_WEIGHTS_WARP) asm volatile("bar.arrive 1, %0;" ::"n"(FP_THREADS) : "memory");
+    else asm volatile("bar.sync 1, %0;" ::"n"(FP_THREADS) : "memory");
+    if constexpr (CG == 2) {
+        asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+        if (warp != FP_WEIGHTS_WARP) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+    }
     tc_fence_after();
-    const uint32_t tmem = sh.tmem;
+    const uint32_t tmem = warp == FP_WEIGHTS_WARP ? 0u : sh.tmem;
 
     if (warp == FP_WEIGHTS_WARP) {
         // ---------------- weights and their scales ----------------
@@ -436,6 +472,7 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
             }
         }
         __syncwarp();
+        if constexpr (CG == 2) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
     } else if (warp == FP_TOKENS_WARP) {
         // ---------------- token rows (of a pair, each CTA's half) and their scales ----------------
         if (lane == 0) {
@@ -513,6 +550,7 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
         FpPiece pc;
         bool ok = true;
         uint32_t uses = 0;
+        int owed = 0, owed_at[2], owed_tile[2], owed_w[2];  // tiles that this warp has to add up (its worker shares two at most)
         walk.start(sh, worker);
         while (ok && walk.next(sh, p, pc)) {
             const int buf = uses & 1;
@@ -573,51 +611,83 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
                 }
             }
             if (!whole) {
-                // the workers that share this tile
-                const long long R = sh.R, G = sh.G;
-                const long long first = walk.u - pc.kb1 - sh.u0, last = first + pc.KB - 1;
-                const int w0 = (int)(((first + 1) * G - 1) / R), w1 = (int)(((last + 1) * G - 1) / R);
+                // The workers that share this tile: those whose shares its first and its last k-block begin in.  (The release that
+                // counts this warp in publishes what it has parked; whoever is last has acquired the others'.)
+                const int c = sh.cost[pc.at], s0 = sh.unit0[pc.at] + pc.tile * pc.KB * c, s1 = s0 + (pc.KB - 1) * c;
+                const float per = (float)sh.G / (float)max(1, sh.unit0[p.E] - sh.u0);
+                int w0 = min(sh.G - 1, (int)((float)(s0 - sh.u0) * per)), w1 = min(sh.G - 1, (int)((float)(s1 - sh.u0) * per));
+                while (sh.cut(w0) > s0) --w0;
+                while (w0 + 1 < sh.G && sh.cut(w0 + 1) <= s0) ++w0;
+                while (sh.cut(w1) > s1) --w1;
+                while (w1 + 1 < sh.G && sh.cut(w1 + 1) <= s1) ++w1;
                 __syncwarp();
                 uint32_t old = 0;
-                if (lane == 0) { __threadfence(); old = count_in(p.counters + (w0 * CG + rank) * FP_EPI_WARPS + warp); __threadfence(); }
+                if (lane == 0) old = count_in(p.counters + (w0 * CG + rank) * FP_EPI_WARPS + warp);
                 old = __shfl_sync(0xFFFFFFFFu, old, 0);
+                // the adding up waits until this worker's other pieces are parked: somebody may be waiting for those
                 if ((int)old == w1 - w0) {
-#pragma unroll 1
-                    for (int k = 0; k < 2 * CG; ++k) {
-                        const int c = (k >> 1) * 128 + half * 64 + (k & 1) * 32, cols = pc.rows - c;
-                        if (cols <= 0) continue;
-                        uint32_t f[32];
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) f[i] = 0;
-                        // two workers' sums on their way at a time, added in the workers' order
-                        for (int q = w0; q <= w1; q += 2) {
-                            const uint4* from = slot_of(q, q == w0) + (c >> 3) * 256;
-                            const uint4* from1 = slot_of(min(q + 1, w1), false) + (c >> 3) * 256;
-                            uint4 a[8], b[8];
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                a[i] = b[i] = make_uint4(0, 0, 0, 0);
-                                if (8 * (i >> 1) < cols) { a[i] = __ldcg(from + i * 128); if (q < w1) b[i] = __ldcg(from1 + i * 128); }
-                            }
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                const int r = 16 * (i & 1) + 4 * (i >> 1);
-                                const uint32_t x[4] = {a[i].x, a[i].y, a[i].z, a[i].w}, y[4] = {b[i].x, b[i].y, b[i].z, b[i].w};
-#pragma unroll
-                                for (int k = 0; k < 4; ++k) f[r + k] = __float_as_uint(__uint_as_float(f[r + k]) + __uint_as_float(x[k]) + __uint_as_float(y[k]));
-                            }
-                        }
-                        int t = to[0][0];
-                        float x = sx[0][0];
-#pragma unroll
-                        for (int i = 1; i < 2 * CG; ++i)
-                            if (i == k) { t = to[i >> 1][i & 1]; x = sx[i >> 1][i & 1]; }
-                        pack_block(f, ow != nullptr, w, x, lane, o);
-                        store_block(p, o, box, t, cols, n0, lane);
-                    }
+                    if (owed == 0) { owed_at[0] = pc.at; owed_tile[0] = pc.tile; owed_w[0] = w0 | w1 << 16; }
+                    else { owed_at[1] = pc.at; owed_tile[1] = pc.tile; owed_w[1] = w0 | w1 << 16; }
+                    ++owed;
                 }
             }
             ++uses;
+        }
+#pragma unroll 1
+        for (int k = 0; ok && k < owed; ++k) {
+            pc.at = k ? owed_at[1] : owed_at[0];
+            pc.tile = k ? owed_tile[1] : owed_tile[0];
+            const int w01 = k ? owed_w[1] : owed_w[0], w0 = w01 & 0xFFFF, w1 = w01 >> 16;
+            place_tile(sh, p.TN, pc);
+            const int j0 = sh.off[pc.e] + pc.i0, n0 = (pc.nt * CG + (int)rank) * 128 + quarter * 32;
+            const float* ow = p.ex[pc.e].outer;
+            const float* ox = p.t.outer + sh.pad0[pc.e] + pc.i0;
+            float w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { const int n = n0 + (lane >> 2) + 8 * i; w[i] = ow && n < p.N ? ow[n] : 1.f; }
+#pragma unroll 1
+            for (int g = 0; g < 2 * CG; ++g) {
+                const int c = (g >> 1) * 128 + half * 64 + (g & 1) * 32, cols = pc.rows - c;
+                if (cols <= 0) continue;
+                const int to = lane < cols ? p.perm[j0 + c + lane] : 0;
+                const float x = ow && lane < cols ? ox[c + lane] : 1.f;
+                auto parked = [&](int q) { return p.partials + ((size_t)(q * CG + rank) * 2 + (q == w0 ? 1 : 0)) * p.TN * 32 + (c >> 3) * 256 + quarter * 32 + lane; };
+                uint32_t f[32], o[16];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) f[i] = 0;
+                auto add = [&](int r, const uint4& a) {
+                    f[r] = __float_as_uint(__uint_as_float(f[r]) + __uint_as_float(a.x)); f[r + 1] = __float_as_uint(__uint_as_float(f[r + 1]) + __uint_as_float(a.y));
+                    f[r + 2] = __float_as_uint(__uint_as_float(f[r + 2]) + __uint_as_float(a.z)); f[r + 3] = __float_as_uint(__uint_as_float(f[r + 3]) + __uint_as_float(a.w));
+                };
+                // several workers' sums on their way at a time, added in the workers' order: four of 16 tokens, two of 32
+                if (cols <= 16) {
+                    for (int q = w0; q <= w1; q += 4) {
+                        uint4 a[4][4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) a[j][i] = q + j <= w1 && 8 * (i >> 1) < cols ? __ldcg(parked(q + j) + i * 128) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) add(16 * (i & 1) + 4 * (i >> 1), a[j][i]);
+                    }
+                } else {
+                    for (int q = w0; q <= w1; q += 2) {
+                        uint4 a[2][8];
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) a[j][i] = q + j <= w1 && 8 * (i >> 1) < cols ? __ldcg(parked(q + j) + i * 128) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) add(16 * (i & 1) + 4 * (i >> 1), a[j][i]);
+                    }
+                }
+                pack_block(f, ow != nullptr, w, x, lane, o);
+                store_block(p, o, box, to, cols, n0, lane);
+            }
         }
     }
 

@@ -6,12 +6,12 @@
 namespace moqe {
 namespace {
 
-template <int FORMAT>
+template <int FORMAT, int CHUNKS>
 __global__ void fp4_rows_kernel(const __nv_bfloat16* __restrict__ X, int K, bool wide, uint8_t* codes, uint8_t* scales, float* outer, __nv_bfloat16* values) {
     __shared__ uint32_t buf[32];
     const size_t m = blockIdx.x;
     const int blocks = (K + fp_block(FORMAT) - 1) / fp_block(FORMAT);
-    encode_row<FORMAT>(X + m * K, K, K, wide, buf, outer ? outer + m : nullptr, [&](int k, uint32_t byte, const uint32_t (&c)[2], int field) {
+    encode_row<FORMAT, CHUNKS>(X + m * K, K, K, wide, buf, outer ? outer + m : nullptr, [&](int k, uint32_t byte, const uint32_t (&c)[2], int field) {
         if (k >= K) return;
         if (codes) {
             uint32_t* to = reinterpret_cast<uint32_t*>(codes + m * (K / 2) + k / 2);
@@ -35,10 +35,10 @@ __global__ void fp4_rows_kernel(const __nv_bfloat16* __restrict__ X, int K, bool
     });
 }
 
-template <int FORMAT>
+template <int FORMAT, int CHUNKS>
 __device__ __forceinline__ void pack_row(const __nv_bfloat16* row, int K, bool wide, const PackedRow& out, float* outer, uint32_t* buf) {
     const int padded = fp_kblocks(K, FORMAT) * 256;
-    encode_row<FORMAT>(row, K, padded, wide, buf, outer, [&](int k, uint32_t byte, const uint32_t (&c)[2], int) { put_packed<FORMAT>(out, k, padded, byte, c); });
+    encode_row<FORMAT, CHUNKS>(row, K, padded, wide, buf, outer, [&](int k, uint32_t byte, const uint32_t (&c)[2], int) { put_packed<FORMAT>(out, k, padded, byte, c); });
 }
 
 struct TokenParams {
@@ -54,6 +54,7 @@ struct TokenParams {
 
 // One block a place j of the sorted order.  The row goes to its place in its expert's segment; segments start at multiples of 128
 // rows.  Places outside [offsets[0], offsets[E]) are nobody's.
+template <int CHUNKS>
 __global__ void fp_tokens_kernel(const __grid_constant__ TokenParams p) {
     __shared__ uint32_t buf[32];
     // the product behind this kernel may read the offset table before this kernel has ended, so nothing is let go before the wait
@@ -73,15 +74,15 @@ __global__ void fp_tokens_kernel(const __grid_constant__ TokenParams p) {
     const __nv_bfloat16* row = p.X + (size_t)from * p.K;
     const int KB = fp_kblocks(p.K, format);
     const PackedRow out = token_row(p.t.codes + pad0 * p.t.row_bytes, p.t.sf + (pad0 >> p.t.sf_shift) * p.t.block_sf, format, i, seg, p.t.sf_shift);
-    if (format == MOQE_FP_MXFP4) pack_row<MOQE_FP_MXFP4>(row, p.K, p.wide, out, nullptr, buf);
-    else if (format == MOQE_FP_NVFP4) pack_row<MOQE_FP_NVFP4>(row, p.K, p.wide, out, p.t.outer + pad0 + i, buf);
+    if (format == MOQE_FP_MXFP4) pack_row<MOQE_FP_MXFP4, CHUNKS>(row, p.K, p.wide, out, nullptr, buf);
+    else if (format == MOQE_FP_NVFP4) pack_row<MOQE_FP_NVFP4, CHUNKS>(row, p.K, p.wide, out, p.t.outer + pad0 + i, buf);
     else {
-        for (int c0 = threadIdx.x; c0 < KB * 4; c0 += blockDim.x * ROW_CHUNKS) {
-            RawBf16 raw[ROW_CHUNKS];
+        for (int c0 = threadIdx.x; c0 < KB * 4; c0 += blockDim.x * CHUNKS) {
+            RawBf16 raw[CHUNKS];
 #pragma unroll
-            for (int i = 0; i < ROW_CHUNKS; ++i) load16(row, (c0 + i * blockDim.x) * 16, p.K, p.wide, raw[i]);
+            for (int i = 0; i < CHUNKS; ++i) load16(row, (c0 + i * blockDim.x) * 16, p.K, p.wide, raw[i]);
 #pragma unroll
-            for (int i = 0; i < ROW_CHUNKS; ++i) {
+            for (int i = 0; i < CHUNKS; ++i) {
                 const int c = 2 * (c0 + i * blockDim.x);
                 const uint32_t* w = raw[i].r.w;
                 if (c >= KB * 8) break;
@@ -92,6 +93,8 @@ __global__ void fp_tokens_kernel(const __grid_constant__ TokenParams p) {
     }
 }
 
+int row_chunks(int M) { return M < 1024 ? 2 : 4; }
+
 }  // namespace
 
 moqe_status launch_fp_tokens(const void* X, const int32_t* perm, const int32_t* offsets, int M, int K, int E, const FpExperts& formats,
@@ -99,12 +102,12 @@ moqe_status launch_fp_tokens(const void* X, const int32_t* perm, const int32_t* 
     const bool wide = K % 16 == 0 && (uintptr_t)X % 32 == 0;
     TokenParams p = {(const __nv_bfloat16*)X, perm, offsets, K, E, wide, tokens, counters, n_counters, formats};
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(M); cfg.blockDim = dim3(row_threads(K)); cfg.stream = st;
+    cfg.gridDim = dim3(M); cfg.blockDim = dim3(row_threads(K, row_chunks(M))); cfg.stream = st;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at; cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, fp_tokens_kernel, p) != cudaSuccess) { cudaGetLastError(); return MOQE_ERR_CUDA; }
+    if (cudaLaunchKernelEx(&cfg, row_chunks(M) == 2 ? fp_tokens_kernel<2> : fp_tokens_kernel<4>, p) != cudaSuccess) { cudaGetLastError(); return MOQE_ERR_CUDA; }
     count_launch();
     return MOQE_OK;
 }
@@ -121,8 +124,10 @@ extern "C" moqe_status moqe_fp4_quantize_rows(const void* X_bf16, int M, int K, 
     if (!X_bf16) return MOQE_ERR_NULL;
     if ((uintptr_t)X_bf16 % 16 || (uintptr_t)values_bf16 % 16 || (uintptr_t)codes % 16 || (uintptr_t)outer % 4) return MOQE_ERR_UNSUPPORTED;
     const bool wide = K % 16 == 0 && (uintptr_t)X_bf16 % 32 == 0 && (uintptr_t)values_bf16 % 32 == 0;
-    const auto kernel = format == MOQE_FP_MXFP4 ? fp4_rows_kernel<MOQE_FP_MXFP4> : fp4_rows_kernel<MOQE_FP_NVFP4>;
-    kernel<<<M, row_threads(K), 0, (cudaStream_t)stream>>>((const __nv_bfloat16*)X_bf16, K, wide, codes, scales, outer, (__nv_bfloat16*)values_bf16);
+    const int chunks = row_chunks(M);
+    const auto kernel = format == MOQE_FP_MXFP4 ? (chunks == 2 ? fp4_rows_kernel<MOQE_FP_MXFP4, 2> : fp4_rows_kernel<MOQE_FP_MXFP4, 4>)
+                                                : (chunks == 2 ? fp4_rows_kernel<MOQE_FP_NVFP4, 2> : fp4_rows_kernel<MOQE_FP_NVFP4, 4>);
+    kernel<<<M, row_threads(K, chunks), 0, (cudaStream_t)stream>>>((const __nv_bfloat16*)X_bf16, K, wide, codes, scales, outer, (__nv_bfloat16*)values_bf16);
     count_launch();
     return cuda_ok(cudaGetLastError());
 }
