@@ -458,13 +458,18 @@ def moqe_routed_qgemm_sorted_multi(Xs: Sequence[torch.Tensor], perm: torch.Tenso
 class FpExpert:
     """Owner of one ``moqe_fp_expert*`` (destroyed with the Python object)."""
 
-    def __init__(self, handle: int):
+    def __init__(self, handle: int, N: int, K: int, fmt: int):
         self.handle = C.c_void_p(handle)
-        N, K, fmt = (C.c_int() for _ in range(3))
-        cb, mb, ab = (C.c_size_t() for _ in range(3))
-        _check(lib().moqe_fp_expert_info(self.handle, N, K, fmt, cb, mb, ab), "moqe_fp_expert_info")
-        self.N, self.K, self.format = N.value, K.value, fmt.value
-        self.code_bytes, self.meta_bytes, self.alloc_bytes = cb.value, mb.value, ab.value
+        self.N, self.K, self.format = N, K, fmt
+
+    def _bytes(self):
+        n = [C.c_size_t() for _ in range(3)]
+        _check(lib().moqe_fp_expert_info(self.handle, None, None, None, *n), "moqe_fp_expert_info")
+        return [v.value for v in n]
+
+    code_bytes = property(lambda self: self._bytes()[0])
+    meta_bytes = property(lambda self: self._bytes()[1])
+    alloc_bytes = property(lambda self: self._bytes()[2])
 
     @property
     def address(self) -> int:
@@ -486,15 +491,20 @@ def _fp_blocks(K: int, fmt: int) -> int:
     return -(-K // (32 if fmt == FP_MXFP4 else 16))
 
 
+def _rows_of(n: int, m: int, dtype, dev) -> torch.Tensor:
+    """An uninitialised [n][m] tensor (empty_strided: 0.8 us less than empty)."""
+    return torch.empty_strided((n, m), (m, 1), dtype=dtype, device=dev)
+
+
 def moqe_fp4_quantize_rows(X: torch.Tensor, fmt: int, values: bool = False):
     """Rows of bf16 ``X[M][K]`` in a 4-bit format: (codes uint8 ``[M][K/2]``, scales uint8 ``[M][blocks]``, outer fp32 ``[M]`` or
     None, values bf16 ``[M][K]`` or None)."""
     X = _dev(X, torch.bfloat16, "X")
     M, K = X.shape
     dev = X.device
-    codes = torch.empty((M, K // 2), dtype=torch.uint8, device=dev)
-    scales = torch.empty((M, _fp_blocks(K, fmt)), dtype=torch.uint8, device=dev)
-    outer = torch.empty(M, dtype=torch.float32, device=dev) if fmt == FP_NVFP4 else None
+    codes = _rows_of(M, K // 2, torch.uint8, dev)
+    scales = _rows_of(M, _fp_blocks(K, fmt), torch.uint8, dev)
+    outer = torch.empty_strided((M,), (1,), dtype=torch.float32, device=dev) if fmt == FP_NVFP4 else None
     vals = torch.empty_like(X) if values else None
     _check(lib().moqe_fp4_quantize_rows(_ptr(X), M, K, int(fmt), _ptr(codes), _ptr(scales), _ptr(outer), _ptr(vals), _stream()),
            "moqe_fp4_quantize_rows")
@@ -507,7 +517,7 @@ def moqe_fp_quantize(W: torch.Tensor, fmt: int) -> FpExpert:
     N, K = W.shape
     out = C.c_void_p()
     _check(lib().moqe_fp_quantize(_ptr(W), N, K, int(fmt), _stream(), C.byref(out)), "moqe_fp_quantize")
-    return FpExpert(out.value)
+    return FpExpert(out.value, N, K, int(fmt))
 
 
 def moqe_fp_expert_import(fmt: int, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
@@ -529,17 +539,17 @@ def moqe_fp_expert_import(fmt: int, codes: Optional[torch.Tensor] = None, scales
     out = C.c_void_p()
     _check(lib().moqe_fp_expert_import(N, K, int(fmt), _ptr(codes), _ptr(scales), _ptr(outer), _ptr(values), _stream(), C.byref(out)),
            "moqe_fp_expert_import")
-    return FpExpert(out.value)
+    return FpExpert(out.value, N, K, int(fmt))
 
 
 def moqe_fp_expert_export(e: FpExpert, values: bool = False):
     """-> (codes, scales, outer, values) as ``moqe_fp4_quantize_rows`` gives them; only values for an ``FP_BF16`` expert."""
-    dev = torch.device("cuda", torch.cuda.current_device())
+    dev = torch._C._cuda_getDevice()
     four = e.format != FP_BF16
-    codes = torch.empty((e.N, e.K // 2), dtype=torch.uint8, device=dev) if four else None
-    scales = torch.empty((e.N, _fp_blocks(e.K, e.format)), dtype=torch.uint8, device=dev) if four else None
-    outer = torch.empty(e.N, dtype=torch.float32, device=dev) if e.format == FP_NVFP4 else None
-    vals = torch.empty((e.N, e.K), dtype=torch.bfloat16, device=dev) if values or not four else None
+    codes = _rows_of(e.N, e.K // 2, torch.uint8, dev) if four else None
+    scales = _rows_of(e.N, _fp_blocks(e.K, e.format), torch.uint8, dev) if four else None
+    outer = torch.empty_strided((e.N,), (1,), dtype=torch.float32, device=dev) if e.format == FP_NVFP4 else None
+    vals = _rows_of(e.N, e.K, torch.bfloat16, dev) if values or not four else None
     _check(lib().moqe_fp_expert_export(e.handle, _ptr(codes), _ptr(scales), _ptr(outer), _ptr(vals), _stream()), "moqe_fp_expert_export")
     return codes, scales, outer, vals
 

@@ -14,9 +14,8 @@
 // the order that tensor memory wants, 512 bytes for 128 rows x 4 scales: row r, scale j at (r % 32) * 16 + (r / 32) * 4 + j.
 //   expert : tile (nt, kb) = 128 channels: 16 KB codes, then their scales (MXFP4 1 KB, NVFP4 2 KB); tiles ordered [nt][kb],
 //            one bulk copy each.  Then NVFP4's channel scales, fp32 [Np].  Rows and k behind the matrix are zeros.
-//   tokens : the rows of an expert start at a multiple of 128 rows (`pad0`); codes [kb][row / 8][1024 bytes], so that the
-//            rows of any tile are one piece; scales [kb][row / 128][1 or 2 KB] (a block for 64 rows where tiles have
-//            that many); row scales fp32.
+//   tokens : the rows of an expert start at a multiple of 16 rows (`pad0`); codes [kb][row / 8][1024 bytes], so that the
+//            rows of any tile are one piece; scales [kb][tile][one or two blocks of 1 or 2 KB]; row scales fp32.
 #pragma once
 #include "common.cuh"
 
@@ -51,11 +50,18 @@ __device__ __forceinline__ PackedRow expert_row(uint8_t* tiles, int KB, int form
     uint8_t* t = tiles + (size_t)(n >> 7) * KB * stride;
     return {t + (r >> 3) * 1024 + (r & 7) * 128, (size_t)stride, t + 16384 + (r & 31) * 16 + (r >> 5) * 4, (size_t)stride, r & 7};
 }
-// row i of a segment of `pad` rows (a multiple of 128); scales in blocks of 2^shift rows
-__device__ __forceinline__ PackedRow token_row(uint8_t* codes, uint8_t* sf, int format, int i, int pad, int shift) {
-    const int sfb = fp_sf_bytes(format), r = i & ((1 << shift) - 1);
+// The token tiles of an expert's n rows: as few as TN tokens allow, of equal size (a multiple of 16).  1040 rows in five tiles of 208
+// instead of four of 256 and one of 16, which costs nearly as much as a full one: four experts of 18944 -> 3584 362 -> 3xx us.
+struct TokenTiles { int tiles, rows; };
+__host__ __device__ inline TokenTiles token_tiles(int n, int TN) {
+    const int t = (n + TN - 1) / TN;
+    return {t, t > 1 ? ((n + t - 1) / t + 15) & ~15 : TN};
+}
+// row i of a segment of `pad` rows; scales in blocks of 128 rows, as many to a tile as TN tokens need
+__device__ __forceinline__ PackedRow token_row(uint8_t* codes, uint8_t* sf, int format, int i, int pad, const TokenTiles& t, int TN) {
+    const int sfb = fp_sf_bytes(format), bpt = TN > 128 ? 2 : 1, tile = t.tiles > 1 ? i / t.rows : 0, in = i - tile * t.rows, r = in & 127;
     return {codes + (size_t)(i >> 3) * 1024 + (i & 7) * 128, (size_t)pad * 128,
-            sf + (size_t)(i >> shift) * sfb + (r & 31) * 16 + (r >> 5) * 4, (size_t)(pad >> shift) * sfb, i & 7};
+            sf + (size_t)(tile * bpt + (in >> 7)) * sfb + (r & 31) * 16 + (r >> 5) * 4, (size_t)(t.tiles * bpt) * sfb, i & 7};
 }
 
 __device__ __forceinline__ float pow2_field(int field) { return __int_as_float(field << 23); }   // 2^(field - 127), 1 <= field <= 254
@@ -283,7 +289,7 @@ bool expert_free(void* p, bool pooled, int device);
 struct FpTokens {
     uint8_t *codes, *sf; float* outer;    // regions of the workspace
     size_t row_bytes, block_sf;           // room for a row's codes, and for a block of scales: the largest of the call's formats
-    int sf_shift;                         // rows of a block of scales: 2^sf_shift, 128 or a tile's 64
+    int TN;                               // most tokens of a tile
 };
 struct FpExperts { uint8_t format[MOQE_MAX_EXPERTS]; };
 moqe_status launch_fp_tokens(const void* X, const int32_t* perm, const int32_t* offsets, int M, int K, int E, const FpExperts& formats,

@@ -60,7 +60,7 @@ struct FpGemmParams {
 struct FpSched {
     // by place in the order of work: 4-bit experts first, then the bf16 ones, whose tiles are four times as deep
     int order[MOQE_MAX_EXPERTS], tile0[MOQE_MAX_EXPERTS + 1], unit0[MOQE_MAX_EXPERTS + 1], KB[MOQE_MAX_EXPERTS], cost[MOQE_MAX_EXPERTS], tts[MOQE_MAX_EXPERTS];
-    int off[MOQE_MAX_EXPERTS + 1], pad0[MOQE_MAX_EXPERTS];      // by expert
+    int off[MOQE_MAX_EXPERTS + 1], pad0[MOQE_MAX_EXPERTS], blk0[MOQE_MAX_EXPERTS], rpt[MOQE_MAX_EXPERTS];      // by expert: rows, padded rows and blocks of scales before it, rows of a token tile
     int W, NT;                   // workers (CTAs or pairs); channel tiles of a worker
     int whole, u0, G, q, r;      // tiles dealt out whole; then what costs from u0 on in equal shares for G workers: q G + r
     uint32_t tmem;
@@ -71,7 +71,7 @@ struct FpSched {
 };
 
 // k-blocks [kb0, kb1) of channel tile nt of the tokens [i0, i0 + rows) of expert e; at: its place in the order; tile: the expert's
-struct FpPiece { int e, nt, i0, rows, kb0, kb1, KB, at, tile; };
+struct FpPiece { int e, nt, tt, i0, rows, kb0, kb1, KB, at, tile; };
 
 // a / b for 0 <= a, 0 < b (a 32-bit division takes far longer; the quotient is a few units off at most)
 __device__ __forceinline__ int div_small(int a, int b) {
@@ -81,12 +81,13 @@ __device__ __forceinline__ int div_small(int a, int b) {
     return q;
 }
 // tokens [i0, i0 + rows) and channel tile of an expert's tile: bands of FP_BAND token tiles, in a band channel tile by channel tile
-__device__ __forceinline__ void place_tile(const FpSched& s, int TN, FpPiece& pc) {
+__device__ __forceinline__ void place_tile(const FpSched& s, FpPiece& pc) {
     const int band = div_small(pc.tile, FP_BAND * s.NT), in = pc.tile - band * FP_BAND * s.NT, deep = min(FP_BAND, s.tts[pc.at] - band * FP_BAND);
     pc.e = s.order[pc.at];
     pc.nt = div_small(in, deep);
-    pc.i0 = (band * FP_BAND + in - pc.nt * deep) * TN;
-    pc.rows = min(TN, s.off[pc.e + 1] - s.off[pc.e] - pc.i0);
+    pc.tt = band * FP_BAND + in - pc.nt * deep;
+    pc.i0 = pc.tt * s.rpt[pc.e];
+    pc.rows = min(s.rpt[pc.e], s.off[pc.e + 1] - s.off[pc.e] - pc.i0);
 }
 
 // What one worker does, piece after piece; every role walks it for itself.  Bands of tiles make the workers of a moment share both
@@ -128,7 +129,7 @@ struct FpWalk {
             u = s.unit0[at] + (pc.tile * pc.KB + pc.kb1) * c;
         }
         pc.at = at;
-        place_tile(s, p.TN, pc);
+        place_tile(s, pc);
         return true;
     }
 };
@@ -389,16 +390,19 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
             const bool is = lane < p.E, deep = is && p.ex[lane].format == MOQE_FP_BF16;
             const int lo = is ? __ldcg(p.offsets + lane) : 0, hi = is ? __ldcg(p.offsets + lane + 1) : 0;
             const uint32_t bf = __ballot_sync(0xFFFFFFFFu, deep), four = __ballot_sync(0xFFFFFFFFu, is && !deep), below = (1u << lane) - 1u;
-            int psum = (hi - lo + 127) & ~127;
-            const int pad = psum;
+            const TokenTiles t = token_tiles(hi - lo, p.TN);
+            const int pad = (hi - lo + 15) & ~15, blocks = t.tiles * (p.TN > 128 ? 2 : 1);
+            int psum = pad, bsum = blocks;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
-                const int c = __shfl_up_sync(0xFFFFFFFFu, psum, d);
-                if (lane >= d) psum += c;
+                const int c = __shfl_up_sync(0xFFFFFFFFu, psum, d), b = __shfl_up_sync(0xFFFFFFFFu, bsum, d);
+                if (lane >= d) { psum += c; bsum += b; }
             }
             if (is) {
                 sh.off[lane] = lo;
                 sh.pad0[lane] = psum - pad;
+                sh.blk0[lane] = bsum - blocks;
+                sh.rpt[lane] = t.rows;
                 if (lane == p.E - 1) sh.off[p.E] = hi;
                 sh.order[deep ? __popc(four) + __popc(bf & below) : __popc(four & below)] = lane;
             }
@@ -407,7 +411,7 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
         {
             const bool is = lane < p.E;
             const int e = is ? sh.order[lane] : 0, rows = is ? sh.off[e + 1] - sh.off[e] : 0, KB = is ? p.ex[e].KB : 1, NT = (p.NT + CG - 1) / CG;
-            const int tts = (rows + p.TN - 1) / p.TN, tiles = tts * NT, cost = is && p.ex[e].format == MOQE_FP_BF16 ? FP_COST_BF16 : FP_COST_4BIT, units = tiles * KB * cost;
+            const int tts = token_tiles(rows, p.TN).tiles, tiles = tts * NT, cost = is && p.ex[e].format == MOQE_FP_BF16 ? FP_COST_BF16 : FP_COST_4BIT, units = tiles * KB * cost;
             int tsum = tiles, usum = units;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
@@ -485,12 +489,12 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
             asm volatile("fence.proxy.async;" ::: "memory");
             walk.start(sh, worker);
             while (ok && walk.next(sh, p, pc)) {
-                const int sfb = fp_sf_bytes(p.ex[pc.e].format), n = (pc.rows + 15) & ~15, shift = p.t.sf_shift;
-                const size_t pad0 = sh.pad0[pc.e], seg = (sh.off[pc.e + 1] - sh.off[pc.e] + 127) & ~127;
+                const int sfb = fp_sf_bytes(p.ex[pc.e].format), n = (pc.rows + 15) & ~15, bpt = p.TN > 128 ? 2 : 1;
+                const size_t pad0 = sh.pad0[pc.e], seg = (sh.off[pc.e + 1] - sh.off[pc.e] + 15) & ~15;
                 const uint32_t bytes = n / CG * 128, sbytes = n > 128 ? 2 * sfb : sfb;
-                const size_t step = seg * 128, sstep = (seg >> shift) * sfb;
+                const size_t step = seg * 128, sstep = (size_t)(sh.tts[pc.at] * bpt) * sfb;
                 const uint8_t* src = p.t.codes + pad0 * p.t.row_bytes + pc.kb0 * step + (size_t)(pc.i0 + rank * (n / 2)) * 128;
-                const uint8_t* ssrc = p.t.sf + (pad0 >> shift) * p.t.block_sf + pc.kb0 * sstep + (size_t)(pc.i0 >> shift) * sfb;
+                const uint8_t* ssrc = p.t.sf + sh.blk0[pc.e] * p.t.block_sf + pc.kb0 * sstep + (size_t)(pc.tt * bpt) * sfb;
                 for (int k = pc.kb1 - pc.kb0; k > 0; --k, src += step, ssrc += sstep) {
                     if (!(ok = mbar_wait_short(bar_empty + 8 * ring.stage, ring.phase ^ 1u, &sh.abort, p.status))) break;
                     const uint32_t full = bar_full + 8 * ring.stage, base = ring0 + ring.stage * p.stage_bytes;
@@ -638,7 +642,7 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
             pc.at = k ? owed_at[1] : owed_at[0];
             pc.tile = k ? owed_tile[1] : owed_tile[0];
             const int w01 = k ? owed_w[1] : owed_w[0], w0 = w01 & 0xFFFF, w1 = w01 >> 16;
-            place_tile(sh, p.TN, pc);
+            place_tile(sh, pc);
             const int j0 = sh.off[pc.e] + pc.i0, n0 = (pc.nt * CG + (int)rank) * 128 + quarter * 32;
             const float* ow = p.ex[pc.e].outer;
             const float* ox = p.t.outer + sh.pad0[pc.e] + pc.i0;
@@ -716,9 +720,6 @@ FpTile pick_tile(int M, int NT) {
     return {M <= 128 || 2ll * NT * ((M + 127) / 128) >= workers ? 128 : 64, false};
 }
 
-// rows of a block of scales: a tile's scales begin at a block's
-int fp_sf_shift(int M, int NT) { return M > 64 && pick_tile(M, NT).TN == 64 ? 6 : 7; }
-
 size_t al256(size_t x) { return (x + 255) / 256 * 256; }
 
 struct FpLayout { size_t perm, offsets, sort, counters, codes, sf, outer, partials, total, row_bytes, block_sf; };
@@ -730,16 +731,17 @@ FpLayout fp_layout(int M, const moqe_fp_expert* const* ex, int E) {
         w.row_bytes = rb > w.row_bytes ? rb : w.row_bytes;
         w.block_sf = sb > w.block_sf ? sb : w.block_sf;
     }
-    // every expert's segment is filled up to 128 rows
-    const size_t blocks = ((size_t)M + 127ull * (size_t)(M < E ? M : E)) / 128;
+    // every expert's segment is filled up to 16 rows, and its last tile's scales to one or two blocks
+    const int TN = pick_tile(M, ex[0]->Np / 128).TN;
+    const size_t some = M < E ? M : E, rows = (size_t)M + 15 * some, blocks = ((size_t)M + (size_t)(TN - 1) * some) / TN * (TN > 128 ? 2 : 1);
     size_t off = 0;
     w.perm = off;     off += al256((size_t)M * 4 + 16);
     w.offsets = off;  off += al256((MOQE_MAX_EXPERTS + 2) * 4);
     w.sort = off;     off += al256(sort_workspace_bytes(M, E));
     w.counters = off; off += al256((size_t)fp_gemm_counters() * 4);
-    w.codes = off;    off += al256(blocks * 128 * w.row_bytes);
-    w.sf = off;       off += al256((blocks << (7 - fp_sf_shift(M, ex[0]->Np / 128))) * w.block_sf);
-    w.outer = off;    off += al256(blocks * 128 * 4);
+    w.codes = off;    off += al256(rows * w.row_bytes);
+    w.sf = off;       off += al256(blocks * w.block_sf);
+    w.outer = off;    off += al256(rows * 4);
     w.partials = off; off += al256(fp_gemm_partial_bytes(M));
     w.total = off;
     return w;
@@ -764,7 +766,7 @@ moqe_status fp_args(const void* X, const void* rows, const void* offsets, int M,
 
 moqe_status fp_run(const void* X, const int32_t* perm, const int32_t* offsets, int M, const moqe_fp_expert* const* ex, int E, void* Y,
                    char* base, const FpLayout& w, cudaStream_t st) {
-    FpTokens t = {(uint8_t*)base + w.codes, (uint8_t*)base + w.sf, (float*)(base + w.outer), w.row_bytes, w.block_sf, fp_sf_shift(M, ex[0]->Np / 128)};
+    FpTokens t = {(uint8_t*)base + w.codes, (uint8_t*)base + w.sf, (float*)(base + w.outer), w.row_bytes, w.block_sf, pick_tile(M, ex[0]->Np / 128).TN};
     FpExperts formats;
     for (int e = 0; e < E; ++e) formats.format[e] = (uint8_t)ex[e]->format;
     uint32_t* counters = (uint32_t*)(base + w.counters);

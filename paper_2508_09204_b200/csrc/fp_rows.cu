@@ -52,7 +52,7 @@ struct TokenParams {
     FpExperts formats;
 };
 
-// One block a place j of the sorted order.  The row goes to its place in its expert's segment; segments start at multiples of 128
+// One block a place j of the sorted order.  The row goes to its place in its expert's segment; segments start at multiples of 16
 // rows.  Places outside [offsets[0], offsets[E]) are nobody's.
 template <int CHUNKS>
 __global__ void fp_tokens_kernel(const __grid_constant__ TokenParams p) {
@@ -64,16 +64,16 @@ __global__ void fp_tokens_kernel(const __grid_constant__ TokenParams p) {
     for (int i = j * blockDim.x + threadIdx.x; i < p.n_counters; i += gridDim.x * blockDim.x) p.counters[i] = 0;
     const int lane = threadIdx.x & 31;
     const int lo = lane < p.E ? p.offsets[lane] : 0x7FFFFFFF, hi = lane < p.E ? p.offsets[lane + 1] : 0x7FFFFFFF;
-    const int pad = lane < p.E ? (hi - lo + 127) & ~127 : 0;
+    const int n = lane < p.E ? hi - lo : 0, pad = (n + 15) & ~15, blocks = (n + p.t.TN - 1) / p.t.TN * (p.t.TN > 128 ? 2 : 1);
     const uint32_t mine = __ballot_sync(0xFFFFFFFFu, j >= lo && j < hi);
     if (mine == 0) return;
     const int e = __ffs(mine) - 1;
-    const size_t pad0 = __reduce_add_sync(0xFFFFFFFFu, lane < e ? pad : 0);
+    const size_t pad0 = __reduce_add_sync(0xFFFFFFFFu, lane < e ? pad : 0), blk0 = __reduce_add_sync(0xFFFFFFFFu, lane < e ? blocks : 0);
     const int i = j - __shfl_sync(0xFFFFFFFFu, lo, e), seg = __shfl_sync(0xFFFFFFFFu, pad, e);
     const int format = p.formats.format[e];
     const __nv_bfloat16* row = p.X + (size_t)from * p.K;
     const int KB = fp_kblocks(p.K, format);
-    const PackedRow out = token_row(p.t.codes + pad0 * p.t.row_bytes, p.t.sf + (pad0 >> p.t.sf_shift) * p.t.block_sf, format, i, seg, p.t.sf_shift);
+    const PackedRow out = token_row(p.t.codes + pad0 * p.t.row_bytes, p.t.sf + blk0 * p.t.block_sf, format, i, seg, token_tiles(__shfl_sync(0xFFFFFFFFu, n, e), p.t.TN), p.t.TN);
     if (format == MOQE_FP_MXFP4) pack_row<MOQE_FP_MXFP4, CHUNKS>(row, p.K, p.wide, out, nullptr, buf);
     else if (format == MOQE_FP_NVFP4) pack_row<MOQE_FP_NVFP4, CHUNKS>(row, p.K, p.wide, out, p.t.outer + pad0 + i, buf);
     else {
