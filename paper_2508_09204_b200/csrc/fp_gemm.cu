@@ -58,16 +58,17 @@ struct FpGemmParams {
 };
 
 struct FpSched {
-    // by place in the order of work: 4-bit experts first, then the bf16 ones, whose tiles are four times as deep
+    // by place in the order of work: bf16 experts first, whose tiles are four times as deep, then the 4-bit ones
     int order[MOQE_MAX_EXPERTS], tile0[MOQE_MAX_EXPERTS + 1], unit0[MOQE_MAX_EXPERTS + 1], KB[MOQE_MAX_EXPERTS], cost[MOQE_MAX_EXPERTS], tts[MOQE_MAX_EXPERTS];
     int off[MOQE_MAX_EXPERTS + 1], pad0[MOQE_MAX_EXPERTS], blk0[MOQE_MAX_EXPERTS], rpt[MOQE_MAX_EXPERTS];      // by expert: rows, padded rows and blocks of scales before it, rows of a token tile
     int W, NT;                   // workers (CTAs or pairs); channel tiles of a worker
-    int whole, u0, G, q, r;      // tiles dealt out whole; then what costs from u0 on in equal shares for G workers: q G + r
+    int whole, u0, G, q, r;      // tiles dealt out whole; then what costs from u0 on in shares for G workers: q G + r in equal ones ...
+    int late, more;              // ... and `more` for each worker from `late` on, who has had a deep tile less
     uint32_t tmem;
     int abort;
     // Where worker w's share begins (u0 and the end of everything for w = 0 and G): a k-block belongs to the share that its start
     // is in.
-    __device__ __forceinline__ int cut(int w) const { return u0 + w * q + (int)((unsigned)(w * r) / (unsigned)G); }
+    __device__ __forceinline__ int cut(int w) const { return u0 + w * q + (int)((unsigned)(w * r) / (unsigned)G) + max(0, w - late) * more; }
 };
 
 // k-blocks [kb0, kb1) of channel tile nt of the tokens [i0, i0 + rows) of expert e; at: its place in the order; tile: the expert's
@@ -404,7 +405,7 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
                 sh.blk0[lane] = bsum - blocks;
                 sh.rpt[lane] = t.rows;
                 if (lane == p.E - 1) sh.off[p.E] = hi;
-                sh.order[deep ? __popc(four) + __popc(bf & below) : __popc(four & below)] = lane;
+                sh.order[deep ? __popc(bf & below) : __popc(bf) + __popc(four & below)] = lane;
             }
         }
         __syncwarp();
@@ -422,23 +423,31 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
                 sh.tile0[lane] = tsum - tiles; sh.unit0[lane] = usum - units; sh.KB[lane] = KB; sh.cost[lane] = cost; sh.tts[lane] = tts;
                 if (lane == p.E - 1) { sh.tile0[p.E] = tsum; sh.unit0[p.E] = usum; }
             }
-            // Rounds of whole tiles; what does not fill a round, and the round before it, are split if that saves more k-blocks than
-            // parking and adding up cost.
+            // There are tiles of two costs, Tb deep ones and T in all.  Whole tiles are dealt out in rounds: their workers go through
+            // the same k together, and find half of what they need in L2.  What is left, at least a tile for each, is cut into
+            // shares that make up for a deep tile less (a pair's 18944 k, 70 bf16 and 210 4-bit tiles on 74 workers: 303 us,
+            // 369 with shares of all but two rounds of 4-bit tiles); if that saves more than parking and adding up cost.
+            const bool is_deep = is && p.ex[e].format == MOQE_FP_BF16;
             const int T = __shfl_sync(0xFFFFFFFFu, tsum, 31), U = __shfl_sync(0xFFFFFFFFu, usum, 31), W = (int)gridDim.x / CG;
-            const uint32_t some = __ballot_sync(0xFFFFFFFFu, tiles > 0);
-            const int last = some ? 31 - __clz(some) : 0, deepest = __shfl_sync(0xFFFFFFFFu, KB * cost, last), left = T % W;
-            const bool alike = __all_sync(0xFFFFFFFFu, tiles == 0 || KB * cost == deepest);
-            int whole = T;
-            if (left != 0 && (long long)deepest * (W - left) > (long long)p.split_cost * FP_COST_BF16 * W) whole = T < W ? 0 : T - left - W;
-            const uint32_t holds = __ballot_sync(0xFFFFFFFFu, is && whole >= tsum - tiles && whole < tsum);
-            const int at = holds ? __ffs(holds) - 1 : 0;
-            const int u0 = whole < T ? __shfl_sync(0xFFFFFFFFu, usum - units + (whole - (tsum - tiles)) * KB * cost, at) : U;
+            const int Tb = __reduce_add_sync(0xFFFFFFFFu, is_deep ? tiles : 0);
+            const int cb = __reduce_max_sync(0xFFFFFFFFu, is_deep && tiles ? KB * cost : 0), cl = __reduce_max_sync(0xFFFFFFFFu, is && !is_deep && tiles ? KB * cost : 0);
+            const int split = p.split_cost * FP_COST_BF16;
             if (lane == 0) {
-                const int R = U - u0;
-                int G = R > 0 ? max(1, min(W, R / (p.least_share * FP_COST_BF16))) : 0;
+                int whole = 0, late = 0, more = 0, R = U, G;
+                const int rounds = (T + W - 1) / W, deep_rounds = (Tb + W - 1) / W;
+                if (T >= W && deep_rounds * cb + (rounds - deep_rounds) * cl <= U / W + split) { whole = T; R = 0; }     // (what the first worker gets)
+                for (int n = T / W; whole == 0 && n > 0; --n) {
+                    const int deep = min(Tb, n * W), rest = U - deep * cb - (n * W - deep) * cl;
+                    const int b = deep < n * W ? deep % W : 0, d = b ? cb - cl : 0;                  // workers from b on have had a deep tile less
+                    if (rest >= W * (cl ? cl : cb) && rest - (W - b) * d >= W * 4 * FP_COST_4BIT) { whole = n * W; R = rest; late = b; more = d; }
+                }
+                G = whole ? W : max(1, min(W, R / (p.least_share * FP_COST_BF16)));
                 // few tiles, all alike: the same number of workers for each, so that nobody has the ends of two, if that is not much longer
-                if (alike && whole == 0 && T <= G && deepest / (G / T) <= R / G + p.split_cost * FP_COST_BF16) G = G / T * T;
-                sh.W = W; sh.NT = NT; sh.whole = whole; sh.u0 = u0; sh.G = G;
+                if (whole == 0 && T > 0 && (Tb == 0 || Tb == T) && T <= G && max(cb, cl) / (G / T) <= R / G + split) G = G / T * T;
+                if (R == 0) G = 0;
+                R -= max(0, G - late) * more;
+                sh.W = W; sh.NT = NT; sh.whole = whole; sh.G = G; sh.late = late; sh.more = more;
+                sh.u0 = whole <= Tb ? whole * cb : Tb * cb + (whole - Tb) * cl;
                 sh.q = G ? R / G : 0; sh.r = G ? R - sh.q * G : 0;
             }
         }
