@@ -61,9 +61,10 @@ struct FpSched {
     // by place in the order of work: bf16 experts first, whose tiles are four times as deep, then the 4-bit ones
     int order[MOQE_MAX_EXPERTS], tile0[MOQE_MAX_EXPERTS + 1], unit0[MOQE_MAX_EXPERTS + 1], KB[MOQE_MAX_EXPERTS], cost[MOQE_MAX_EXPERTS], tts[MOQE_MAX_EXPERTS];
     int off[MOQE_MAX_EXPERTS + 1], pad0[MOQE_MAX_EXPERTS], blk0[MOQE_MAX_EXPERTS], rpt[MOQE_MAX_EXPERTS];      // by expert: rows, padded rows and blocks of scales before it, rows of a token tile
-    int W, NT;                   // workers (CTAs or pairs); channel tiles of a worker
-    int whole, u0, G, q, r;      // tiles dealt out whole; then what costs from u0 on in shares for G workers: q G + r in equal ones ...
-    int late, more;              // ... and `more` for each worker from `late` on, who has had a deep tile less
+    int W, NT, all_deep;         // workers (CTAs or pairs); channel tiles of a worker; tiles of bf16 experts
+    int deep, light;             // tiles dealt out whole: of bf16 experts; of 4-bit ones, behind all of those
+    int late, extra;             // workers from `late` on, who have a deep tile less, have `extra` rounds of light ones before the others
+    int u0, G, q, r, more;       // what costs from u0 on in shares for G workers: q G + r in equal ones, `more` for each from `late` on
     uint32_t tmem;
     int abort;
     // Where worker w's share begins (u0 and the end of everything for w = 0 and G): a k-block belongs to the share that its start
@@ -95,21 +96,25 @@ __device__ __forceinline__ void place_tile(const FpSched& s, FpPiece& pc) {
 // token and weight tiles in L2.  Whole tiles go to the workers in turn; the rest are one sequence of k-blocks, cut into shares of
 // equal cost (a 4-bit k-block brings scales, and its tiles are short).
 struct FpWalk {
-    int at, t, u, ue;
-    __device__ __forceinline__ void start(const FpSched& s, int w) {
-        at = 0;
-        t = w;
+    int at, w, phase, t, u, ue;
+    __device__ __forceinline__ void start(const FpSched& s, int worker) {
+        at = phase = 0;
+        t = w = worker;
         u = ue = 0;
         if (w < s.G) { u = s.cut(w); ue = s.cut(w + 1); }
     }
     __device__ __forceinline__ bool next(const FpSched& s, const FpGemmParams& p, FpPiece& pc) {
-        if (t < s.whole) {
-            while (t >= s.tile0[at + 1]) ++at;
-            pc.tile = t - s.tile0[at];
+        if (phase == 0 && t >= s.deep) { phase = 1; t = w >= s.late ? w - s.late : s.light; }
+        if (phase == 1 && t >= min(s.light, s.extra * (s.W - s.late))) { phase = 2; t = s.extra * (s.W - s.late) + w; }
+        if (phase == 2 && t >= s.light) phase = 3;
+        if (phase < 3) {
+            const int tile = phase == 0 ? t : s.all_deep + t;
+            while (tile >= s.tile0[at + 1]) ++at;
+            pc.tile = tile - s.tile0[at];
             pc.KB = s.KB[at];
             pc.kb0 = 0;
             pc.kb1 = pc.KB;
-            t += s.W;
+            t += phase == 1 ? s.W - s.late : s.W;
         } else {
             // (u, ue: in costs; the k-blocks that begin in [u, ue))
             int c, v, end;
@@ -257,13 +262,13 @@ __device__ __forceinline__ void issue_piece(FpIssue& q, const FpGemmParams& p, u
     const int sets = SCARCE ? 2 : p.stages;
     const uint32_t id0 = FORMAT == MOQE_FP_BF16 ? idesc_bf16<CG>(n) : idesc_fp4<CG>(n, FORMAT == MOQE_FP_MXFP4, 0);
     if (FORMAT != MOQE_FP_BF16 && q.format != FORMAT) {
-        // sets of another size: everything before must have been multiplied
+        // sets of another size, or none for a while: everything before must have been multiplied
         if (q.format != 0) q.ok &= mbar_wait_short(bar_empty + 8 * q.last.stage, q.last.phase, abort_flag, p.status);
-        q.format = FORMAT;
         q.set = 0;
         q.fresh = sets;
         q.behind = q.ring;
     }
+    q.format = FORMAT;
     for (int k = 0; k < kblocks; k += TURN) {
         const Ring r0 = q.ring;
         Ring r1 = r0;
@@ -278,7 +283,7 @@ __device__ __forceinline__ void issue_piece(FpIssue& q, const FpGemmParams& p, u
         __syncwarp();
         tc_fence_after();
         const uint32_t a0 = ring0 + r0.stage * p.stage_bytes, a1 = ring0 + r1.stage * p.stage_bytes;
-        const int set1 = q.set + 1 == sets ? 0 : q.set + 1;
+        const int set1 = q.set + 1 >= sets ? 0 : q.set + 1;
         if (elect_one()) {
             issue_kblock<CG, FORMAT>(d, a0, p.b_off, p.sfb_off, sf0 + q.set * SET, id0, n, k == 0);
             fp_commit<CG>(bar_empty + 8 * r0.stage);
@@ -423,31 +428,37 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
                 sh.tile0[lane] = tsum - tiles; sh.unit0[lane] = usum - units; sh.KB[lane] = KB; sh.cost[lane] = cost; sh.tts[lane] = tts;
                 if (lane == p.E - 1) { sh.tile0[p.E] = tsum; sh.unit0[p.E] = usum; }
             }
-            // There are tiles of two costs, Tb deep ones and T in all.  Whole tiles are dealt out in rounds: their workers go through
-            // the same k together, and find half of what they need in L2.  What is left, at least a tile for each, is cut into
-            // shares that make up for a deep tile less (a pair's 18944 k, 70 bf16 and 210 4-bit tiles on 74 workers: 303 us,
-            // 369 with shares of all but two rounds of 4-bit tiles); if that saves more than parking and adding up cost.
+            // There are tiles of two costs: Tb deep ones (bf16) and Tl light ones.  Dealt out whole, their workers go through the same k
+            // together and find half of what they need in L2; a worker without the last round's deep tile gets as many light ones
+            // more as make up for it.  If that leaves too many without work, what does not fill a round of whole tiles, at least a
+            // tile for each, is cut into shares that make up for a deep tile less (a pair's 18944 k, 70 bf16 and 210 4-bit tiles on
+            // 74 workers: 303 us, 369 with shares of all but two rounds of 4-bit tiles).
             const bool is_deep = is && p.ex[e].format == MOQE_FP_BF16;
             const int T = __shfl_sync(0xFFFFFFFFu, tsum, 31), U = __shfl_sync(0xFFFFFFFFu, usum, 31), W = (int)gridDim.x / CG;
-            const int Tb = __reduce_add_sync(0xFFFFFFFFu, is_deep ? tiles : 0);
+            const int Tb = __reduce_add_sync(0xFFFFFFFFu, is_deep ? tiles : 0), Tl = T - Tb, rb = Tb / W, b = Tb - rb * W;
             const int cb = __reduce_max_sync(0xFFFFFFFFu, is_deep && tiles ? KB * cost : 0), cl = __reduce_max_sync(0xFFFFFFFFu, is && !is_deep && tiles ? KB * cost : 0);
             const int split = p.split_cost * FP_COST_BF16;
+            // all whole, `lane` rounds of light tiles for everybody: how many more for those without the last deep one, and how long it takes
+            const int few = b ? (rb + 1) * cb : 0, short_of = max(0, Tl - lane * W), rounds = (short_of + W - b - 1) / (W - b);
+            const int takes = max(few + (b ? lane * cl : 0), rb * cb + (lane + rounds) * cl);
+            const int best = __reduce_min_sync(0xFFFFFFFFu, takes), who = __ffs(__ballot_sync(0xFFFFFFFFu, takes == best)) - 1;
+            const int extra_best = __shfl_sync(0xFFFFFFFFu, rounds, who);
             if (lane == 0) {
-                int whole = 0, late = 0, more = 0, R = U, G;
-                const int rounds = (T + W - 1) / W, deep_rounds = (Tb + W - 1) / W;
-                if (T >= W && deep_rounds * cb + (rounds - deep_rounds) * cl <= U / W + split) { whole = T; R = 0; }     // (what the first worker gets)
+                int whole = 0, extra = 0, late = 0, more = 0, R = U, G;
+                if (T >= W && best <= U / W + split) { whole = T; extra = extra_best; late = b; R = 0; }
                 for (int n = T / W; whole == 0 && n > 0; --n) {
                     const int deep = min(Tb, n * W), rest = U - deep * cb - (n * W - deep) * cl;
-                    const int b = deep < n * W ? deep % W : 0, d = b ? cb - cl : 0;                  // workers from b on have had a deep tile less
-                    if (rest >= W * (cl ? cl : cb) && rest - (W - b) * d >= W * 4 * FP_COST_4BIT) { whole = n * W; R = rest; late = b; more = d; }
+                    const bool uneven = deep < n * W && b > 0;                  // workers from b on have had a deep tile less
+                    const int d = uneven ? cb - cl : 0;
+                    if (rest >= W * (cl ? cl : cb) && rest - (W - b) * d >= W * 4 * FP_COST_4BIT) { whole = n * W; R = rest; late = uneven ? b : 0; extra = uneven; more = d; }
                 }
                 G = whole ? W : max(1, min(W, R / (p.least_share * FP_COST_BF16)));
                 // few tiles, all alike: the same number of workers for each, so that nobody has the ends of two, if that is not much longer
                 if (whole == 0 && T > 0 && (Tb == 0 || Tb == T) && T <= G && max(cb, cl) / (G / T) <= R / G + split) G = G / T * T;
                 if (R == 0) G = 0;
+                sh.W = W; sh.NT = NT; sh.all_deep = Tb; sh.deep = min(Tb, whole); sh.light = whole - sh.deep; sh.late = late; sh.extra = extra; sh.more = more;
+                sh.u0 = sh.deep * cb + sh.light * cl; sh.G = G;
                 R -= max(0, G - late) * more;
-                sh.W = W; sh.NT = NT; sh.whole = whole; sh.G = G; sh.late = late; sh.more = more;
-                sh.u0 = whole <= Tb ? whole * cb : Tb * cb + (whole - Tb) * cl;
                 sh.q = G ? R / G : 0; sh.r = G ? R - sh.q * G : 0;
             }
         }
@@ -495,7 +506,6 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
             bool ok = true;
             asm volatile("griddepcontrol.wait;" ::: "memory");
             asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-            asm volatile("fence.proxy.async;" ::: "memory");
             walk.start(sh, worker);
             while (ok && walk.next(sh, p, pc)) {
                 const int sfb = fp_sf_bytes(p.ex[pc.e].format), n = (pc.rows + 15) & ~15, bpt = p.TN > 128 ? 2 : 1;
