@@ -445,14 +445,14 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
             const int extra_best = __shfl_sync(0xFFFFFFFFu, rounds, who);
             if (lane == 0) {
                 int whole = 0, extra = 0, late = 0, more = 0, R = U, G;
-                if (T >= W && best <= U / W + split) { whole = T; extra = extra_best; late = b; R = 0; }
+                if (T > 0 && best <= U / W + split) { whole = T; extra = extra_best; late = b; R = 0; }
                 for (int n = T / W; whole == 0 && n > 0; --n) {
                     const int deep = min(Tb, n * W), rest = U - deep * cb - (n * W - deep) * cl;
                     const bool uneven = deep < n * W && b > 0;                  // workers from b on have had a deep tile less
                     const int d = uneven ? cb - cl : 0;
                     if (rest >= W * (cl ? cl : cb) && rest - (W - b) * d >= W * 4 * FP_COST_4BIT) { whole = n * W; R = rest; late = uneven ? b : 0; extra = uneven; more = d; }
                 }
-                G = whole ? W : max(1, min(W, R / (p.least_share * FP_COST_BF16)));
+                G = whole ? W : max(max(1, min(T, W)), min(W, R / (p.least_share * FP_COST_BF16)));
                 // few tiles, all alike: the same number of workers for each, so that nobody has the ends of two, if that is not much longer
                 if (whole == 0 && T > 0 && (Tb == 0 || Tb == T) && T <= G && max(cb, cl) / (G / T) <= R / G + split) G = G / T * T;
                 if (R == 0) G = 0;
@@ -824,8 +824,8 @@ moqe_status launch_fp_gemm(const moqe_fp_expert* const* ex, int E, int M, const 
     // (one SM, NVFP4: eight sets of 32 columns behind two accumulators of 128)
     if (!pair && p.stages > 8) p.stages = 8;
     static_assert(FP_RING_BYTES / (16384 + 1024 + 16384 + 2048) <= 5, "a pair has room for five sets of 24 columns");
-    p.split_cost = pair ? 18 : 6;
-    p.least_share = pair ? 16 : 4;
+    p.split_cost = pair ? 36 : 20;
+    p.least_share = pair ? 24 : 12;
     static std::atomic<unsigned long long> attr[2] = {};
     const auto kernel = pair ? fp_gemm_kernel<2> : fp_gemm_kernel<1>;
     if (!ensure_dynamic_smem((const void*)kernel, FP_SMEM, attr[pair])) { cudaGetLastError(); return MOQE_ERR_CUDA; }
