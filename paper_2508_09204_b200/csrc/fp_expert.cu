@@ -1,5 +1,5 @@
-// Floating-point experts: built from fp32 weights, imported from and exported to canonical arrays.  One block a channel (see
-// encode_row).
+// Floating-point experts: built from fp32 weights, imported from and exported to canonical arrays.  One block or warp
+// a channel (see encode_row).
 #include <new>
 
 #include "fp_formats.cuh"
@@ -8,14 +8,15 @@ namespace moqe {
 namespace {
 
 template <int FORMAT>
-__global__ void fp_build_kernel(const float* __restrict__ W, int N, int K, int KB, bool wide, uint8_t* tiles, float* outer) {
+__global__ void fp_build_kernel(const float* __restrict__ W, int N, int K, int KB, bool wide, bool warps, uint8_t* tiles, float* outer) {
     __shared__ uint32_t buf[32];
-    const int n = blockIdx.x, padded = KB * fp_kbk(FORMAT);
+    const RowPlace at = row_place(warps);                  // (channels are a multiple of a block's)
+    const int n = at.row, padded = KB * fp_kbk(FORMAT);
     const PackedRow out = expert_row(tiles, KB, FORMAT, n);
     const float* row = W + (size_t)n * K;
     const int have = n < N ? K : 0;                         // channels behind the last are zeros
     if constexpr (FORMAT == MOQE_FP_BF16) {
-        for (int k = threadIdx.x * 16; k < padded; k += blockDim.x * 16) {
+        for (int k = at.tid * 16; k < padded; k += at.nt * 16) {
             RawF32 raw;
             load16(row, k, have, wide, raw);
             float x[16];
@@ -26,7 +27,7 @@ __global__ void fp_build_kernel(const float* __restrict__ W, int N, int K, int K
                     make_uint4(pack_bf16x2(x[8 * h], x[8 * h + 1]), pack_bf16x2(x[8 * h + 2], x[8 * h + 3]), pack_bf16x2(x[8 * h + 4], x[8 * h + 5]), pack_bf16x2(x[8 * h + 6], x[8 * h + 7]));
         }
     } else {
-        encode_row<FORMAT, 2>(row, have, padded, wide, buf, outer ? outer + n : nullptr, [&](int k, uint32_t byte, const uint32_t (&c)[2], int) { put_packed<FORMAT>(out, k, padded, byte, c); });
+        encode_row<FORMAT, 2>(row, have, padded, wide, at.tid, at.nt, buf, outer ? outer + n : nullptr, [&](int k, uint32_t byte, const uint32_t (&c)[2], int) { put_packed<FORMAT>(out, k, padded, byte, c); });
     }
 }
 
@@ -132,7 +133,8 @@ extern "C" moqe_status moqe_fp_quantize(const float* W, int N, int K, int format
     moqe_fp_expert* e = nullptr;
     if ((s = fp_alloc(N, K, format, st, &e)) != MOQE_OK) return s;
     const auto kernel = format == MOQE_FP_MXFP4 ? fp_build_kernel<MOQE_FP_MXFP4> : format == MOQE_FP_NVFP4 ? fp_build_kernel<MOQE_FP_NVFP4> : fp_build_kernel<MOQE_FP_BF16>;
-    kernel<<<e->Np, row_threads(K, 2), 0, st>>>(W, N, K, e->KB, (uintptr_t)W % 32 == 0, e->tiles, e->outer);
+    const RowLaunch l = row_launch(e->Np, K, 2);
+    kernel<<<l.blocks, l.threads, 0, st>>>(W, N, K, e->KB, (uintptr_t)W % 32 == 0, row_threads(K, 2) == 32, e->tiles, e->outer);
     count_launch();
     if (cudaGetLastError() != cudaSuccess) { moqe_fp_expert_destroy(e); return MOQE_ERR_CUDA; }
     *out = e;

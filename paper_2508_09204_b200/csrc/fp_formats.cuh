@@ -221,15 +221,15 @@ __device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t* buf) {
     return __reduce_max_sync(0xFFFFFFFFu, v);
 }
 
-// One row by the whole block: every chunk of the `padded` k is encoded and handed to `sink(k, byte, codes, field)` by all lanes of its
+// One row by `nt` threads, a whole block or one of its warps (then `tid` is the lane): every chunk of the `padded` k is encoded and handed to `sink(k, byte, codes, field)` by all lanes of its
 // warp together; NVFP4's row scale comes first (from registers where the row fits into them, else the row is read twice).
 // `wide`: rows begin on 32-byte boundaries.
 template <class T> struct RawOf { typedef RawBf16 type; };
 template <> struct RawOf<float> { typedef RawF32 type; };
 template <int FORMAT, int CHUNKS, class T, class Sink>
-__device__ __forceinline__ void encode_row(const T* row, int have, int padded, bool wide, uint32_t* buf, float* outer, Sink sink) {
+__device__ __forceinline__ void encode_row(const T* row, int have, int padded, bool wide, int tid, int nt, uint32_t* buf, float* outer, Sink sink) {
     constexpr bool FP32 = sizeof(T) == 4;
-    const int span = blockDim.x * 16 * CHUNKS, parts = (padded + span - 1) / span, k0 = threadIdx.x * 16, step = blockDim.x * 16;
+    const int span = nt * 16 * CHUNKS, parts = (padded + span - 1) / span, k0 = tid * 16, step = nt * 16;
     typename RawOf<T>::type raw[CHUNKS];
     int field = 127;
     if constexpr (FORMAT == MOQE_FP_NVFP4) {
@@ -240,8 +240,8 @@ __device__ __forceinline__ void encode_row(const T* row, int have, int padded, b
 #pragma unroll
             for (int i = 0; i < CHUNKS; ++i) { float x[16]; widen(raw[i], x); m = max(m, finite_amax16(x)); }
         }
-        field = nv_row_field(block_max(m, buf));
-        if (outer && threadIdx.x == 0) *outer = pow2_field(field);
+        field = nv_row_field(nt == 32 ? __reduce_max_sync(0xFFFFFFFFu, m) : block_max(m, buf));
+        if (outer && tid == 0) *outer = pow2_field(field);
     }
     for (int part = 0; part < parts; ++part) {
         if (FORMAT != MOQE_FP_NVFP4 || parts > 1) {
@@ -262,10 +262,22 @@ __device__ __forceinline__ void encode_row(const T* row, int have, int padded, b
         }
     }
 }
-// Threads of a block that takes a row, so that the row fits into their registers if it can.
+// Threads that take a row, so that the row fits into their registers if it can; rows of a block: four where a warp is enough.
 inline int row_threads(int K, int chunks) {
     const int t = ((K + 15) / 16 + chunks - 1) / chunks;
     return t >= 512 ? 512 : (t + 31) / 32 * 32;
+}
+constexpr int ROWS_OF_WARPS = 4;
+struct RowLaunch { int blocks, threads; };
+inline RowLaunch row_launch(int rows, int K, int chunks) {
+    const int t = row_threads(K, chunks);
+    return t > 32 ? RowLaunch{rows, t} : RowLaunch{(rows + ROWS_OF_WARPS - 1) / ROWS_OF_WARPS, 32 * ROWS_OF_WARPS};
+}
+// which row this thread works on, as which of how many threads
+struct RowPlace { int row, tid, nt; };
+__device__ __forceinline__ RowPlace row_place(bool warps) {
+    if (warps) return {(int)(blockIdx.x * ROWS_OF_WARPS + (threadIdx.x >> 5)), (int)(threadIdx.x & 31), 32};
+    return {(int)blockIdx.x, (int)threadIdx.x, (int)blockDim.x};
 }
 // ... into a packed row: four scales to a store.  (All lanes of a warp; `padded` is a multiple of 256, so half warps are there as a whole.)
 template <int FORMAT>

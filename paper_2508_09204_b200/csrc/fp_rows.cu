@@ -1,5 +1,5 @@
 // Rows of activations in the microscaled 4-bit formats: canonical arrays for the caller (moqe_fp4_quantize_rows), and the packed
-// token rows of a routed product.  One block a row (see encode_row).  Bound by HBM: 2 bytes a number are
+// token rows of a routed product.  One block or warp a row (see encode_row).  Bound by HBM: 2 bytes a number are
 // read, half a byte and the scales written.
 #include "fp_formats.cuh"
 
@@ -7,11 +7,13 @@ namespace moqe {
 namespace {
 
 template <int FORMAT, int CHUNKS>
-__global__ void fp4_rows_kernel(const __nv_bfloat16* __restrict__ X, int K, bool wide, uint8_t* codes, uint8_t* scales, float* outer, __nv_bfloat16* values) {
+__global__ void fp4_rows_kernel(const __nv_bfloat16* __restrict__ X, int M, int K, bool wide, bool warps, uint8_t* codes, uint8_t* scales, float* outer, __nv_bfloat16* values) {
     __shared__ uint32_t buf[32];
-    const size_t m = blockIdx.x;
+    const RowPlace at = row_place(warps);
+    if (at.row >= M) return;
+    const size_t m = at.row;
     const int blocks = (K + fp_block(FORMAT) - 1) / fp_block(FORMAT);
-    encode_row<FORMAT, CHUNKS>(X + m * K, K, K, wide, buf, outer ? outer + m : nullptr, [&](int k, uint32_t byte, const uint32_t (&c)[2], int field) {
+    encode_row<FORMAT, CHUNKS>(X + m * K, K, K, wide, at.tid, at.nt, buf, outer ? outer + m : nullptr, [&](int k, uint32_t byte, const uint32_t (&c)[2], int field) {
         if (k >= K) return;
         if (codes) {
             uint32_t* to = reinterpret_cast<uint32_t*>(codes + m * (K / 2) + k / 2);
@@ -36,23 +38,23 @@ __global__ void fp4_rows_kernel(const __nv_bfloat16* __restrict__ X, int K, bool
 }
 
 template <int FORMAT, int CHUNKS>
-__device__ __forceinline__ void pack_row(const __nv_bfloat16* row, int K, bool wide, const PackedRow& out, float* outer, uint32_t* buf) {
+__device__ __forceinline__ void pack_row(const __nv_bfloat16* row, int K, bool wide, const RowPlace& at, const PackedRow& out, float* outer, uint32_t* buf) {
     const int padded = fp_kblocks(K, FORMAT) * 256;
-    encode_row<FORMAT, CHUNKS>(row, K, padded, wide, buf, outer, [&](int k, uint32_t byte, const uint32_t (&c)[2], int) { put_packed<FORMAT>(out, k, padded, byte, c); });
+    encode_row<FORMAT, CHUNKS>(row, K, padded, wide, at.tid, at.nt, buf, outer, [&](int k, uint32_t byte, const uint32_t (&c)[2], int) { put_packed<FORMAT>(out, k, padded, byte, c); });
 }
 
 struct TokenParams {
     const __nv_bfloat16* X;
     const int32_t *perm, *offsets;
-    int K, E;
-    bool wide;
+    int M, K, E;
+    bool wide, warps;
     FpTokens t;
     uint32_t* counters;
     int n_counters;
     FpExperts formats;
 };
 
-// One block a place j of the sorted order.  The row goes to its place in its expert's segment; segments start at multiples of 16
+// One block, or one warp of it, a place j of the sorted order.  The row goes to its place in its expert's segment; segments start at multiples of 16
 // rows.  Places outside [offsets[0], offsets[E]) are nobody's.
 template <int CHUNKS>
 __global__ void fp_tokens_kernel(const __grid_constant__ TokenParams p) {
@@ -60,9 +62,11 @@ __global__ void fp_tokens_kernel(const __grid_constant__ TokenParams p) {
     // the product behind this kernel may read the offset table before this kernel has ended, so nothing is let go before the wait
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int j = blockIdx.x, from = p.perm[j];
-    for (int i = j * blockDim.x + threadIdx.x; i < p.n_counters; i += gridDim.x * blockDim.x) p.counters[i] = 0;
-    const int lane = threadIdx.x & 31;
+    const RowPlace at = row_place(p.warps);
+    const int j = at.row;
+    for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < p.n_counters; i += gridDim.x * blockDim.x) p.counters[i] = 0;
+    if (j >= p.M) return;
+    const int lane = threadIdx.x & 31, from = p.perm[j];
     const int lo = lane < p.E ? p.offsets[lane] : 0x7FFFFFFF, hi = lane < p.E ? p.offsets[lane + 1] : 0x7FFFFFFF;
     const int n = lane < p.E ? hi - lo : 0, pad = (n + 15) & ~15, blocks = (n + p.t.TN - 1) / p.t.TN * (p.t.TN > 128 ? 2 : 1);
     const uint32_t mine = __ballot_sync(0xFFFFFFFFu, j >= lo && j < hi);
@@ -74,16 +78,16 @@ __global__ void fp_tokens_kernel(const __grid_constant__ TokenParams p) {
     const __nv_bfloat16* row = p.X + (size_t)from * p.K;
     const int KB = fp_kblocks(p.K, format);
     const PackedRow out = token_row(p.t.codes + pad0 * p.t.row_bytes, p.t.sf + blk0 * p.t.block_sf, format, i, seg, token_tiles(__shfl_sync(0xFFFFFFFFu, n, e), p.t.TN), p.t.TN);
-    if (format == MOQE_FP_MXFP4) pack_row<MOQE_FP_MXFP4, CHUNKS>(row, p.K, p.wide, out, nullptr, buf);
-    else if (format == MOQE_FP_NVFP4) pack_row<MOQE_FP_NVFP4, CHUNKS>(row, p.K, p.wide, out, p.t.outer + pad0 + i, buf);
+    if (format == MOQE_FP_MXFP4) pack_row<MOQE_FP_MXFP4, CHUNKS>(row, p.K, p.wide, at, out, nullptr, buf);
+    else if (format == MOQE_FP_NVFP4) pack_row<MOQE_FP_NVFP4, CHUNKS>(row, p.K, p.wide, at, out, p.t.outer + pad0 + i, buf);
     else {
-        for (int c0 = threadIdx.x; c0 < KB * 4; c0 += blockDim.x * CHUNKS) {
+        for (int c0 = at.tid; c0 < KB * 4; c0 += at.nt * CHUNKS) {
             RawBf16 raw[CHUNKS];
 #pragma unroll
-            for (int i = 0; i < CHUNKS; ++i) load16(row, (c0 + i * blockDim.x) * 16, p.K, p.wide, raw[i]);
+            for (int i = 0; i < CHUNKS; ++i) load16(row, (c0 + i * at.nt) * 16, p.K, p.wide, raw[i]);
 #pragma unroll
             for (int i = 0; i < CHUNKS; ++i) {
-                const int c = 2 * (c0 + i * blockDim.x);
+                const int c = 2 * (c0 + i * at.nt);
                 const uint32_t* w = raw[i].r.w;
                 if (c >= KB * 8) break;
                 *reinterpret_cast<uint4*>(out.chunk(c >> 3, c & 7)) = make_uint4(w[0], w[1], w[2], w[3]);
@@ -100,9 +104,10 @@ int row_chunks(int M) { return M < 1024 ? 2 : 4; }
 moqe_status launch_fp_tokens(const void* X, const int32_t* perm, const int32_t* offsets, int M, int K, int E, const FpExperts& formats,
                              const FpTokens& tokens, uint32_t* counters, int n_counters, cudaStream_t st) {
     const bool wide = K % 16 == 0 && (uintptr_t)X % 32 == 0;
-    TokenParams p = {(const __nv_bfloat16*)X, perm, offsets, K, E, wide, tokens, counters, n_counters, formats};
+    TokenParams p = {(const __nv_bfloat16*)X, perm, offsets, M, K, E, wide, row_threads(K, row_chunks(M)) == 32, tokens, counters, n_counters, formats};
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(M); cfg.blockDim = dim3(row_threads(K, row_chunks(M))); cfg.stream = st;
+    const RowLaunch l = row_launch(M, K, row_chunks(M));
+    cfg.gridDim = dim3(l.blocks); cfg.blockDim = dim3(l.threads); cfg.stream = st;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
@@ -127,7 +132,8 @@ extern "C" moqe_status moqe_fp4_quantize_rows(const void* X_bf16, int M, int K, 
     const int chunks = row_chunks(M);
     const auto kernel = format == MOQE_FP_MXFP4 ? (chunks == 2 ? fp4_rows_kernel<MOQE_FP_MXFP4, 2> : fp4_rows_kernel<MOQE_FP_MXFP4, 4>)
                                                 : (chunks == 2 ? fp4_rows_kernel<MOQE_FP_NVFP4, 2> : fp4_rows_kernel<MOQE_FP_NVFP4, 4>);
-    kernel<<<M, row_threads(K, chunks), 0, (cudaStream_t)stream>>>((const __nv_bfloat16*)X_bf16, K, wide, codes, scales, outer, (__nv_bfloat16*)values_bf16);
+    const RowLaunch l = row_launch(M, K, chunks);
+    kernel<<<l.blocks, l.threads, 0, (cudaStream_t)stream>>>((const __nv_bfloat16*)X_bf16, M, K, wide, row_threads(K, chunks) == 32, codes, scales, outer, (__nv_bfloat16*)values_bf16);
     count_launch();
     return cuda_ok(cudaGetLastError());
 }
