@@ -312,9 +312,9 @@ moqe_status launch_fp_gemm(const moqe_fp_expert* const* ex, int E, int M, const 
                            uint32_t* counters, void* partials, void* Y, cudaStream_t st);
 int fp_gemm_counters();
 
-// fp_gemv.cu: batches of one row
+// fp_gemv.cu: batches of one row, or a few of a small layer
 bool fp_gemv_supported(const moqe_fp_expert* const* ex, int E, int M);
-moqe_status launch_fp_gemv(const void* X, const int32_t* perm, const int32_t* offsets, const moqe_fp_expert* const* ex, int E, void* Y, cudaStream_t st);
+moqe_status launch_fp_gemv(const void* X, int M, const int32_t* perm, const int32_t* offsets, const moqe_fp_expert* const* ex, int E, void* Y, cudaStream_t st);
 size_t fp_gemm_partial_bytes(int M);
 
 }  // namespace moqe

@@ -785,7 +785,7 @@ moqe_status fp_args(const void* X, const void* rows, const void* offsets, int M,
 
 moqe_status fp_run(const void* X, const int32_t* perm, const int32_t* offsets, int M, const moqe_fp_expert* const* ex, int E, void* Y,
                    char* base, const FpLayout& w, cudaStream_t st) {
-    if (fp_gemv_supported(ex, E, M)) return launch_fp_gemv(X, perm, offsets, ex, E, Y, st);
+    if (fp_gemv_supported(ex, E, M)) return launch_fp_gemv(X, M, perm, offsets, ex, E, Y, st);
     FpTokens t = {(uint8_t*)base + w.codes, (uint8_t*)base + w.sf, (float*)(base + w.outer), w.row_bytes, w.block_sf, pick_tile(M, ex[0]->Np / 128).TN};
     FpExperts formats;
     for (int e = 0; e < E; ++e) formats.format[e] = (uint8_t)ex[e]->format;

@@ -1,10 +1,11 @@
-// Routed product of floating-point experts for ONE row (a single sequence's decode step): one launch, weights read once.
+// Routed product of floating-point experts for one row (a single sequence's decode step), and for a few of a small layer: one launch, a
+// row's weights read once.
 //
-//   Y[perm[0]][n] = bf16( o_x o_w[n] sum_b sx[b] sw[n][b] sum_{k in b} cx[k] cw[n][k] )
+//   Y[perm[j]][n] = bf16( o_x o_w[n] sum_b sx[b] sw[n][b] sum_{k in b} cx[k] cw[n][k] )
 //
 // Bound by HBM: 4.25 or 4.5 bits a weight.  The tensor-core kernel needs the row quantized by a kernel before it, splits few tiles along k
 // and adds parked sums up, which is most of its time here (4096 channels x 11008 k: 12.6 us, of which 3.7 are the bytes'; this
-// kernel 7.x).  So a block of 4 to 16 warps takes 32 channels and all of k: nothing is added up outside the block, and every block
+// kernel 8.6).  So a block of 4 to 16 warps takes 32 channels and all of k: nothing is added up outside the block, and every block
 // quantizes the row for itself while its first weights are on their way.
 //
 // A 4-bit number doubled is a whole number, {0, 1, 2, 3, 4, 6, 8, 12} and a sign, so that the products of a block of codes are
@@ -179,9 +180,9 @@ __global__ void __launch_bounds__(GEMV_THREADS, 1) fp_gemv_kernel(const __grid_c
     __shared__ float sums[GEMV_WARPS][32];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    // the row's expert: whose segment holds place 0, if any does
-    const int lane = threadIdx.x & 31, from = p.perm[0];
-    const uint32_t mine = __ballot_sync(0xFFFFFFFFu, lane < p.E && p.offsets[min(lane, p.E - 1)] <= 0 && p.offsets[min(lane, p.E - 1) + 1] > 0);
+    // the row's expert: whose segment holds its place, if any does
+    const int lane = threadIdx.x & 31, at = min(lane, p.E - 1), place = blockIdx.y, from = p.perm[place];
+    const uint32_t mine = __ballot_sync(0xFFFFFFFFu, lane < p.E && p.offsets[at] <= place && p.offsets[at + 1] > place);
     if (mine == 0) return;
     const GemvExpert& x = p.ex[__ffs(mine) - 1];
     if (x.format == MOQE_FP_MXFP4) gemv<MOQE_FP_MXFP4>(p, x, from, smem, buf, sums);
@@ -200,9 +201,17 @@ size_t gemv_smem(const moqe_fp_expert* const* ex, int E) {
 
 }  // namespace
 
-bool fp_gemv_supported(const moqe_fp_expert* const* ex, int E, int M) { return M == 1 && gemv_smem(ex, E) <= (size_t)GEMV_SMEM_MAX; }
+// One row; or rows that a block each for 32 channels takes less time for than the 4 us that the tensor-core kernel and the one before it
+// need to get going.  A block costs as much as 530 k of its channels.  This kernel / the other, us:
+//   4096 x 4096  4-bit: 1 row 4.6 / 10.4, 2 rows 7.1 / 10.3, 3 rows 10.7 / 10.3;  with a bf16 expert: 2 rows 10 / 18
+//   1024 x 1024  4-bit: 4 rows 3.9 / 7.5, 16 rows 5.1 / 7.5, 32 rows 7.5 / 7.5;  with a bf16 expert: 16 rows 4.7 / 9.8
+//   512 x 512    4-bit: 64 rows 6.2 / 6.7, 128 rows 11.2 / 7.1;   11008 x 4096, 2 rows: 14.7 / 10.5
+bool fp_gemv_supported(const moqe_fp_expert* const* ex, int E, int M) {
+    if (gemv_smem(ex, E) > (size_t)GEMV_SMEM_MAX) return false;
+    return M == 1 || (long long)M * ex[0]->Np * (ex[0]->K + 530ll) <= 49000000;
+}
 
-moqe_status launch_fp_gemv(const void* X, const int32_t* perm, const int32_t* offsets, const moqe_fp_expert* const* ex, int E, void* Y, cudaStream_t st) {
+moqe_status launch_fp_gemv(const void* X, int M, const int32_t* perm, const int32_t* offsets, const moqe_fp_expert* const* ex, int E, void* Y, cudaStream_t st) {
     GemvParams p = {};
     for (int e = 0; e < E; ++e) p.ex[e] = {ex[e]->tiles, ex[e]->outer, ex[e]->format, ex[e]->KB};
     p.X = (const __nv_bfloat16*)X; p.perm = perm; p.offsets = offsets; p.Y = (__nv_bfloat16*)Y;
@@ -212,9 +221,9 @@ moqe_status launch_fp_gemv(const void* X, const int32_t* perm, const int32_t* of
     if (!ensure_dynamic_smem((const void*)fp_gemv_kernel, GEMV_SMEM_MAX, attr)) { cudaGetLastError(); return MOQE_ERR_CUDA; }
     cudaLaunchConfig_t cfg = {};
     // all blocks at once, if they are not too many: 4, 2 or 1 to an SM (344 blocks of 16 warps, three after one another on an SM: 16.3 us
-    // for 11008 channels x 4096 k, with 4 warps xx)
-    const int blocks = ex[0]->Np / 32, sms = device_sm_count(), warps = blocks <= sms ? GEMV_WARPS : blocks <= 2 * sms ? 8 : 4;
-    cfg.gridDim = dim3(blocks); cfg.blockDim = dim3(32 * warps); cfg.dynamicSmemBytes = gemv_smem(ex, E); cfg.stream = st;
+    // for 11008 channels x 4096 k, with 4 warps 11.3)
+    const int blocks = ex[0]->Np / 32 * M, sms = device_sm_count(), warps = blocks <= sms ? GEMV_WARPS : blocks <= 2 * sms ? 8 : 4;
+    cfg.gridDim = dim3(ex[0]->Np / 32, M); cfg.blockDim = dim3(32 * warps); cfg.dynamicSmemBytes = gemv_smem(ex, E); cfg.stream = st;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;

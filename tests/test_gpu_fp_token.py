@@ -1,4 +1,5 @@
-"""One row through the floating-point experts (a sequence's decode step): every format, short and long rows, odd sizes."""
+"""One row through the floating-point experts (a sequence's decode step), and a few of a small layer: every format, short and long rows,
+odd sizes."""
 import numpy as np
 import pytest
 import torch
@@ -22,6 +23,25 @@ def test_shapes(fmt, N, K):
     assert moqe.moqe_async_status() == moqe.OK
     _check(Y, X, ids, [w], [fmt])
     assert torch.equal(Y, moqe.moqe_routed_fpgemm(X, ids, [e]))
+
+
+@pytest.mark.parametrize("M,N,K,formats", [(2, 4096, 1024, [MX, NV]), (5, 1000, 264, [BF, NV, MX]), (16, 264, 1032, [NV, MX, NV]), (64, 520, 136, [MX, BF]),
+                                           (200, 8, 64, [NV, MX, BF]), (33, 136, 72, [MX] * 31 + [NV])])
+def test_a_few_rows(M, N, K, formats):
+    g = np.random.default_rng(M)
+    ex = [_expert(M + e, N, K, f) for e, f in enumerate(formats)]
+    X = _bf16(g.standard_normal((M, K)))
+    ids = _dev(g.integers(-1, len(formats) + 1, M).astype(np.int32))
+    Y = moqe.moqe_routed_fpgemm(X, ids, [e for e, _ in ex])
+    moqe.moqe_async_status()
+    _check(Y, X, ids, [w for _, w in ex], formats)
+    assert bool((Y[(ids < 0) | (ids >= len(formats))] == 0).all())
+    _, perm, offsets = moqe.moqe_permute(None, ids, len(formats))
+    moqe.moqe_async_status()
+    Z = torch.full_like(Y, 4.0)
+    ws = moqe.alloc_workspace(moqe.moqe_routed_fpgemm_workspace(M, [ex[1][0]]))
+    moqe.moqe_routed_fpgemm_sorted(X, perm, offsets[1:3], [ex[1][0]], Z, ws)
+    assert torch.equal(Z[ids == 1], Y[ids == 1]) and bool((Z[ids != 1] == 4).all())
 
 
 def test_routing():
