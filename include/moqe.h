@@ -343,6 +343,7 @@ MOQE_API moqe_status moqe_routed_qgemm_workspace_clear(void* workspace, size_t w
  *            and codes 0; the other blocks of its row are as without it.
  * Canonical arrays: codes [rows][K / 2], two a byte, the even k in the low half; scales [rows][ceil(K / 32 or 16)], one byte each;
  * outer fp32 [rows] (NVFP4 only); values bf16 [rows][K] = code * scale * outer, rounded once.  K % 8 == 0.
+ * Beyond K = 2^24, 2^30 rows or output channels, or M N K = 2^49 in a product, calls may be refused (MOQE_ERR_UNSUPPORTED).
  * ------------------------------------------------------------------------- */
 typedef enum { MOQE_FP_MXFP4 = 1, MOQE_FP_NVFP4 = 2, MOQE_FP_BF16 = 3 } moqe_fp_format;
 
@@ -380,7 +381,7 @@ MOQE_API moqe_status moqe_fp_expert_destroy(moqe_fp_expert* e);
 
 /* The routed product, grouped by expert with ragged sizes, from one row to whole prompts:
  *   Y[m][n] = bf16( sum_k xq[m][k] * w_e[n][k] ),   e = row_ids[m]
- * with fp32 sums.  xq = the row quantized to the format of ITS expert (the values of moqe_fp4_quantize_rows) where that is a 4-bit
+ * with fp32 sums (of code * scale; an outer scale of the channel, then the row's, is applied to the sum).  xq = the row quantized to the format of ITS expert (the values of moqe_fp4_quantize_rows) where that is a 4-bit
  * format -- both operands have 4 bits and go to the tensor cores with their scales -- and the row itself where it is BF16.
  * The experts of a call may have any mixture of formats; they agree on N (a multiple of 8) and K.  The same call gives the
  * same bits.  workspace: moqe_routed_fpgemm_workspace(M, h_experts, E) bytes (0 for refused arguments), 256-byte aligned, contents

@@ -97,7 +97,7 @@ __global__ void fp_export_kernel(uint8_t* tiles, const float* outer, int K, int 
 
 moqe_status fp_check(int N, int K, int format) {
     if (N <= 0 || K <= 0) return MOQE_ERR_SHAPE;
-    if (format < MOQE_FP_MXFP4 || format > MOQE_FP_BF16 || K % 8 != 0) return MOQE_ERR_UNSUPPORTED;
+    if (format < MOQE_FP_MXFP4 || format > MOQE_FP_BF16 || K % 8 != 0 || K > FP_MAX_K || N > FP_MAX_N) return MOQE_ERR_UNSUPPORTED;
     return MOQE_OK;
 }
 

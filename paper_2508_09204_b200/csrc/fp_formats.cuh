@@ -31,6 +31,7 @@ struct moqe_fp_expert {
 
 namespace moqe {
 
+constexpr int FP_MAX_K = 1 << 24, FP_MAX_N = 1 << 30;      // (indices within a row and numbers of rows are 32-bit)
 __host__ __device__ inline int fp_block(int format) { return format == MOQE_FP_MXFP4 ? 32 : 16; }       // k that share a scale
 __host__ __device__ inline int fp_kbk(int format) { return format == MOQE_FP_BF16 ? 64 : 256; }         // k of a k-block
 __host__ __device__ inline int fp_sf_bytes(int format) { return format == MOQE_FP_MXFP4 ? 1024 : format == MOQE_FP_NVFP4 ? 2048 : 0; }   // scales of 128 rows, a k-block
@@ -221,8 +222,8 @@ __device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t* buf) {
     return __reduce_max_sync(0xFFFFFFFFu, v);
 }
 
-// One row by `nt` threads, a whole block or one of its warps (then `tid` is the lane): every chunk of the `padded` k is encoded and handed to `sink(k, byte, codes, field)` by all lanes of its
-// warp together; NVFP4's row scale comes first (from registers where the row fits into them, else the row is read twice).
+// One row by `nt` threads, a whole block or one of its warps (then `tid` is the lane): every chunk of the `padded` k is encoded and
+// handed to `sink(k, byte, codes, field)` by all lanes of its warp together; NVFP4's row scale comes first (from registers where the row fits into them, else the row is read twice).
 // `wide`: rows begin on 32-byte boundaries.
 template <class T> struct RawOf { typedef RawBf16 type; };
 template <> struct RawOf<float> { typedef RawF32 type; };
@@ -311,10 +312,10 @@ moqe_status launch_fp_tokens(const void* X, const int32_t* perm, const int32_t* 
 moqe_status launch_fp_gemm(const moqe_fp_expert* const* ex, int E, int M, const int32_t* perm, const int32_t* offsets, const FpTokens& tokens,
                            uint32_t* counters, void* partials, void* Y, cudaStream_t st);
 int fp_gemm_counters();
+size_t fp_gemm_partial_bytes(int M);
 
 // fp_gemv.cu: batches of one row, or a few of a small layer
 bool fp_gemv_supported(const moqe_fp_expert* const* ex, int E, int M);
 moqe_status launch_fp_gemv(const void* X, int M, const int32_t* perm, const int32_t* offsets, const moqe_fp_expert* const* ex, int E, void* Y, cudaStream_t st);
-size_t fp_gemm_partial_bytes(int M);
 
 }  // namespace moqe

@@ -2,19 +2,25 @@
 //
 //   Y[perm[j]][n] = bf16( o_x[j] o_w[n] sum_k x[j][k] w_e[n][k] ),  e = the expert whose segment holds j
 //
-// 128 channels are the rows of an MMA (TMEM lanes), up to 128 tokens its columns, so that single tokens and prompts are the same
-// code: only the columns shrink.  The tensor cores multiply the 4-bit codes and their block scales as they are
+// 128 channels (two SMs: 256) are the rows of an MMA (TMEM lanes), up to 128 (256) tokens its columns, so that a few tokens and prompts
+// are the same code: only the columns shrink.  The tensor cores multiply the 4-bit codes and their block scales as they are
 // (tcgen05.mma kind::mxf4nvf4, 64 k to an instruction); bf16 experts use kind::f16 with 16 k.  Either way an instruction takes
 // 32 bytes of a row, so a k-block of 128 bytes a row is four instructions of about the same duration, whatever the format, and is
 // the unit that work is split by.
 //
-// One CTA to an SM.  Two warps (one lane each) fill a ring of stages with bulk copies: weights with their scales (one copy), which
-// do not wait for the kernel that quantizes the rows; token rows and their scales (two).  One warp (one elected lane) copies scales
-// to tensor memory and issues the MMAs into one of two accumulators; eight warps read the other one, a thread a channel, scale,
-// round and store.  Work: whole tiles dealt out in turn where there are plenty; else, and for what is left over, the tiles' k-blocks
-// in one sequence, an equal share to every worker ("stream-K").  A warp that holds part of a tile parks its fp32 sums and counts
-// itself in; the last one adds them up in the order of the workers, so that a call gives the same bits every time.  Nobody waits
-// for another worker.
+// One CTA to an SM; a worker is a CTA or a pair.  Two warps (one lane each) fill a ring of stages with bulk copies: weights with their
+// scales (one copy), which do not wait for the kernel that quantizes the rows; token rows and their scales (two).  One warp (one elected
+// lane) copies scales to tensor memory and issues the MMAs into one of two accumulators; eight warps read the other one, 32 channels
+// x 64 tokens each at a time, scale, round, turn them round with matrix stores and write 64 bytes a token.  Work: whole tiles
+// dealt out in turn where there are plenty; else, and for what is left over, the tiles' k-blocks in one sequence, an equal share to
+// every worker.  A warp that holds part of a tile parks its fp32 sums and counts itself in; the last one adds them up in the
+// order of the workers, so that a call gives the same bits every time.  Nobody waits for another worker.
+//
+// Bound by HBM up to some 100 rows an expert (16 rows, 4096 -> 11008, three formats: 139.9 MB in 28.3 us with the kernel before it,
+// 76 % of the copy rate), by the tensor cores beyond (8192 x 4096 x 4096: bf16 178 us, 1540 TFLOP/s; MXFP4 59.7 us, 4600; NVFP4 67.6 us,
+// 4070).  A 4-bit k-block of a pair takes 512 cycles at the least; a turn of the issuing warp is about as long with NVFP4 (12
+// copies of scales and 4 MMAs: 580 cycles), and the first k-blocks of a tile wait until half of the last accumulator has been read (1600
+// of a tile's 9800 cycles at k = 4096).
 //
 // Every mbarrier wait is bounded; on expiry the CTA raises its abort flag, latches MOQE_ERR_TIMEOUT, lets copies in flight land,
 // frees its tensor memory and returns.
@@ -343,7 +349,7 @@ __device__ __forceinline__ void pack_block(const uint32_t* v, bool scaled, const
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
             float lo = __uint_as_float(v[16 * (b >> 1) + 4 * j + 2 * (b & 1)]), hi = __uint_as_float(v[16 * (b >> 1) + 4 * j + 2 * (b & 1) + 1]);
-            if (scaled) { lo *= w[b] * x0; hi *= w[b] * x1; }
+            if (scaled) { lo = lo * w[b] * x0; hi = hi * w[b] * x1; }
             o[4 * j + b] = pack_bf16(lo, hi);
         }
     }
@@ -494,6 +500,8 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
                     ring.advance(p.stages);
                 }
             }
+            // (the last stages are handed back by arrivals from the tensor cores, a pair's second CTA's from the first: they land here)
+            for (int i = 0; ok && i < p.stages; ++i, ring.advance(p.stages)) ok = mbar_wait_short(bar_empty + 8 * ring.stage, ring.phase ^ 1u, &sh.abort, p.status);
         }
         __syncwarp();
         if constexpr (CG == 2) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
@@ -564,7 +572,7 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
         }
         __syncwarp();
     } else {
-        // ---------------- epilogue: thread = channel = TMEM lane; two warps to a quarter of the lanes, 64 tokens at a time ----------------
+        // ---------------- epilogue: two warps to a quarter of the channels (TMEM lanes), 64 tokens each at a time ----------------
         asm volatile("griddepcontrol.wait;" ::: "memory");
         const int quarter = warp & 3, half = warp >> 2;
         const uint32_t box = ring0 + FP_RING_BYTES + warp * FP_BOX;
@@ -730,13 +738,33 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
     }
 }
 
-// Tokens of a tile, and whether two SMs share it.
+// Tokens of a tile, and whether two SMs share it.  Up to 64 rows a tile is as narrow as the batch.  A pair reads weights and tokens half as
+// often, but its tiles are four times as large: it gets them if there are at least half as many of them as pairs (4096 -> 4096: 2048 rows
+// MXFP4 28.2 us, with one SM to a tile 35.1, 600 rows 15.3 and 17.6, 8192 rows bf16 238 and 312; 4096 -> 1024, 2048 rows in NVFP4 and bf16
+// 38.3 with pairs, 34.0 without).  One SM's tiles take 64 tokens instead of 128 where the larger ones would leave SMs without and a call
+// has both kinds of experts, bf16 ones four times as deep (777 rows, 2056 -> 1000, three formats: 16.5 us, with 128 tokens 20.7;
+// 4-bit experts only 12.5 and 11.9, bf16 only 19.8 and 19.4 (512 channels of 3584 k)).
 struct FpTile { int TN; bool pair; };
-FpTile pick_tile(int M, int NT) {
+FpTile pick_tile(int M, const moqe_fp_expert* const* ex, int E) {
     if (M <= 64) return {M <= 16 ? 16 : M <= 32 ? 32 : 64, false};
-    const long long workers = device_sm_count();
-    if (M > 128 && 4ll * ((NT + 1) / 2) * ((M + 255) / 256) >= workers) return {256, true};
-    return {M <= 128 || 2ll * NT * ((M + 127) / 128) >= workers ? 128 : 64, false};
+    const long long workers = device_sm_count(), NT = ex[0]->Np / 128;
+    if (M > 128 && 4 * ((NT + 1) / 2) * ((M + 255ll) / 256) >= workers) return {256, true};
+    int deep = 0;
+    for (int e = 0; e < E; ++e) deep += ex[e]->format == MOQE_FP_BF16;
+    return {M <= 128 || deep == 0 || deep == E || 2 * NT * ((M + 127ll) / 128) >= workers ? 128 : 64, false};
+}
+
+// The schedule counts costs in 32 bits.
+bool fp_schedulable(int M, const moqe_fp_expert* const* ex, int E) {
+    if (M > 1 << 30) return false;
+    long long deepest = 0;
+    for (int e = 0; e < E; ++e) {
+        const long long cost = (long long)ex[e]->KB * (ex[e]->format == MOQE_FP_BF16 ? FP_COST_BF16 : FP_COST_4BIT);
+        deepest = cost > deepest ? cost : deepest;
+    }
+    const FpTile t = pick_tile(M, ex, E);
+    const long long tiles = ((long long)M / t.TN + E) * (t.pair ? (ex[0]->Np / 128 + 1) / 2 : ex[0]->Np / 128);
+    return tiles <= (1ll << 30) / deepest;
 }
 
 size_t al256(size_t x) { return (x + 255) / 256 * 256; }
@@ -750,9 +778,9 @@ FpLayout fp_layout(int M, const moqe_fp_expert* const* ex, int E) {
         w.row_bytes = rb > w.row_bytes ? rb : w.row_bytes;
         w.block_sf = sb > w.block_sf ? sb : w.block_sf;
     }
-    // every expert's segment is filled up to 16 rows, and its last tile's scales to one or two blocks
-    const int TN = pick_tile(M, ex[0]->Np / 128).TN;
-    const size_t some = M < E ? M : E, rows = (size_t)M + 15 * some, blocks = ((size_t)M + (size_t)(TN - 1) * some) / TN * (TN > 128 ? 2 : 1);
+    // Every expert's segment is filled up to 16 rows, its last tile's scales to a block or two.  (Whatever the tile, there are no more
+    // blocks than these: a workspace for many rows serves fewer ones.)
+    const size_t some = M < E ? M : E, rows = (size_t)M + 15 * some, blocks = (size_t)M / 64 + 2 * some + 1;
     size_t off = 0;
     w.perm = off;     off += al256((size_t)M * 4 + 16);
     w.offsets = off;  off += al256((MOQE_MAX_EXPERTS + 2) * 4);
@@ -777,7 +805,7 @@ moqe_status fp_args(const void* X, const void* rows, const void* offsets, int M,
         if (ex[e]->N != ex[0]->N || ex[e]->K != ex[0]->K) return MOQE_ERR_MISMATCH;
     if (M == 0) return MOQE_OK;
     if (!X || !rows || !offsets || !Y) return MOQE_ERR_NULL;
-    if (ex[0]->N % 8 != 0 || (uintptr_t)X % 16 || (uintptr_t)Y % 16) return MOQE_ERR_UNSUPPORTED;
+    if (ex[0]->N % 8 != 0 || (uintptr_t)X % 16 || (uintptr_t)Y % 16 || !fp_schedulable(M, ex, E)) return MOQE_ERR_UNSUPPORTED;
     w = fp_layout(M, ex, E);
     if (!workspace || workspace_bytes < w.total || (uintptr_t)workspace % 256) return MOQE_ERR_WORKSPACE;
     return MOQE_OK;
@@ -786,7 +814,7 @@ moqe_status fp_args(const void* X, const void* rows, const void* offsets, int M,
 moqe_status fp_run(const void* X, const int32_t* perm, const int32_t* offsets, int M, const moqe_fp_expert* const* ex, int E, void* Y,
                    char* base, const FpLayout& w, cudaStream_t st) {
     if (fp_gemv_supported(ex, E, M)) return launch_fp_gemv(X, M, perm, offsets, ex, E, Y, st);
-    FpTokens t = {(uint8_t*)base + w.codes, (uint8_t*)base + w.sf, (float*)(base + w.outer), w.row_bytes, w.block_sf, pick_tile(M, ex[0]->Np / 128).TN};
+    FpTokens t = {(uint8_t*)base + w.codes, (uint8_t*)base + w.sf, (float*)(base + w.outer), w.row_bytes, w.block_sf, pick_tile(M, ex, E).TN};
     FpExperts formats;
     for (int e = 0; e < E; ++e) formats.format[e] = (uint8_t)ex[e]->format;
     uint32_t* counters = (uint32_t*)(base + w.counters);
@@ -813,7 +841,7 @@ moqe_status launch_fp_gemm(const moqe_fp_expert* const* ex, int E, int M, const 
     p.status = device_status_word();
     if (!p.status) return MOQE_ERR_ALLOC;
     p.E = E; p.N = ex[0]->N; p.NT = ex[0]->Np / 128;
-    const FpTile tile = pick_tile(M, p.NT);
+    const FpTile tile = pick_tile(M, ex, E);
     const bool pair = tile.pair;
     p.TN = tile.TN;
     // a stage: weights, their scales, token rows (from a multiple of 1024), their scales
@@ -825,6 +853,9 @@ moqe_status launch_fp_gemm(const moqe_fp_expert* const* ex, int E, int M, const 
     // (one SM, NVFP4: eight sets of 32 columns behind two accumulators of 128)
     if (!pair && p.stages > 8) p.stages = 8;
     static_assert(FP_RING_BYTES / (16384 + 1024 + 16384 + 2048) <= 5, "a pair has room for five sets of 24 columns");
+    // One SM's sums are parked and added up in some 20 k-blocks' time, a pair's (four times as many) in 36.  With 6 and 18 instead:
+    // 48 rows of NVFP4, 4096 -> 11008, 18.9 us for 12.5; 512 rows in three formats 32 for 28.5; 4160 rows of 3584 -> 18944 295 for 285;
+    // 2048 rows of bf16 62 for 59.
     p.split_cost = pair ? 36 : 20;
     p.least_share = pair ? 24 : 12;
     static std::atomic<unsigned long long> attr[2] = {};
@@ -851,7 +882,7 @@ extern "C" size_t moqe_routed_fpgemm_workspace(int M, const moqe_fp_expert* cons
     if (M < 0 || !h_experts || E <= 0 || E > MOQE_MAX_EXPERTS) return 0;
     for (int e = 0; e < E; ++e)
         if (!h_experts[e]) return 0;
-    return fp_layout(M, h_experts, E).total;
+    return fp_schedulable(M, h_experts, E) ? fp_layout(M, h_experts, E).total : 0;
 }
 
 extern "C" moqe_status moqe_routed_fpgemm_sorted(const void* X_bf16, const int32_t* perm, const int32_t* offsets, int M,

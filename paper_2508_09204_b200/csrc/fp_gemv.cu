@@ -71,6 +71,8 @@ __device__ __forceinline__ float2 e4m3_pair(uint32_t two) {
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)(two & 0x7F7Fu)));
     return __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
+// (a product of two scales that fp32 does not hold may still meet a sum of zero)
+__device__ __forceinline__ float finite_or_nan(float s) { float d; asm("min.NaN.f32 %0, %1, 0f7F7FFFFF;" : "=f"(d) : "f"(s)); return d; }
 __device__ __forceinline__ uint32_t word_of(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
 // act: the row as signed bytes (4-bit formats: doubled numbers) or bf16, 256 or 128 bytes a k-block; sx: its blocks' scales
@@ -102,7 +104,7 @@ __device__ __forceinline__ void add_block(const GemvBlock& b, const unsigned cha
                 const uint32_t s = word_of(b.sf[h], j);
                 if constexpr (FORMAT == MOQE_FP_MXFP4) {
                     const int sum = dot8(w.x, a0.x, a0.y, dot8(w.y, a0.z, a0.w, dot8(w.z, a1.x, a1.y, dot8(w.w, a1.z, a1.w, 0))));
-                    acc[j][h] = fmaf((float)sum, e8m0_value((s >> (8 * (c & 3))) & 255u) * s1, acc[j][h]);
+                    acc[j][h] = fmaf((float)sum, finite_or_nan(e8m0_value((s >> (8 * (c & 3))) & 255u) * s1), acc[j][h]);
                 } else {
                     const int lo = dot8(w.x, a0.x, a0.y, dot8(w.y, a0.z, a0.w, 0)), hi = dot8(w.z, a1.x, a1.y, dot8(w.w, a1.z, a1.w, 0));
                     const float2 sw = e4m3_pair(s >> (16 * (c & 1)));
@@ -140,7 +142,7 @@ __device__ __forceinline__ void gemv(const GemvParams& p, const GemvExpert& x, i
             }
             *reinterpret_cast<uint4*>(smem + k) = make_uint4(o[0], o[1], o[2], o[3]);
             if (FORMAT == MOQE_FP_NVFP4) sx[k >> 4] = e4m3_value(byte);
-            else if ((k & 16) == 0) sx[k >> 5] = e8m0_value(byte);
+            else if ((k & 16) == 0) sx[k >> 5] = 0.25f * e8m0_value(byte);                 // (both factors are doubled)
         });
         ox = pow2_field(f);
     }
@@ -167,8 +169,8 @@ __device__ __forceinline__ void gemv(const GemvParams& p, const GemvExpert& x, i
         for (int w = 0; w < warps; ++w) s += sums[w][threadIdx.x];
         const int n = nt * 128 + 32 * (threadIdx.x >> 3) + 8 * q + (threadIdx.x & 7);
         if (n < p.N) {
-            if constexpr (FORMAT != MOQE_FP_BF16) s *= 0.25f;                            // (both factors are doubled)
-            if constexpr (FORMAT == MOQE_FP_NVFP4) s *= x.outer[n] * ox;
+            if constexpr (FORMAT == MOQE_FP_NVFP4) s *= 0.25f;                           // (both factors are doubled)
+            if constexpr (FORMAT == MOQE_FP_NVFP4) s = s * x.outer[n] * ox;
             p.Y[(size_t)from * p.N + n] = __float2bfloat16_rn(s);
         }
     }

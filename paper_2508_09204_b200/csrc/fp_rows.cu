@@ -54,8 +54,8 @@ struct TokenParams {
     FpExperts formats;
 };
 
-// One block, or one warp of it, a place j of the sorted order.  The row goes to its place in its expert's segment; segments start at multiples of 16
-// rows.  Places outside [offsets[0], offsets[E]) are nobody's.
+// One block, or one warp of it, a place j of the sorted order.  The row goes to its place in its expert's segment; segments start at
+// multiples of 16 rows.  Places outside [offsets[0], offsets[E]) are nobody's.
 template <int CHUNKS>
 __global__ void fp_tokens_kernel(const __grid_constant__ TokenParams p) {
     __shared__ uint32_t buf[32];
@@ -124,7 +124,7 @@ using namespace moqe;
 extern "C" moqe_status moqe_fp4_quantize_rows(const void* X_bf16, int M, int K, int format, uint8_t* codes, uint8_t* scales, float* outer,
                                               void* values_bf16, void* stream) {
     if (M < 0 || K <= 0) return MOQE_ERR_SHAPE;
-    if ((format != MOQE_FP_MXFP4 && format != MOQE_FP_NVFP4) || K % 8 != 0) return MOQE_ERR_UNSUPPORTED;
+    if ((format != MOQE_FP_MXFP4 && format != MOQE_FP_NVFP4) || K % 8 != 0 || K > FP_MAX_K) return MOQE_ERR_UNSUPPORTED;
     if (M == 0) return MOQE_OK;
     if (!X_bf16) return MOQE_ERR_NULL;
     if ((uintptr_t)X_bf16 % 16 || (uintptr_t)values_bf16 % 16 || (uintptr_t)codes % 16 || (uintptr_t)outer % 4) return MOQE_ERR_UNSUPPORTED;

@@ -56,6 +56,15 @@ def test_experts(L):
     assert L.moqe_fp_expert_destroy(None) == moqe.ERR_NULL
 
 
+def test_sizes_beyond_the_indices(L):
+    out = C.c_void_p()
+    for N, K in ((8, (1 << 24) + 8), (8, (1 << 31) - 8), ((1 << 30) + 1, 64), ((1 << 31) - 1, 64)):
+        for fmt in (moqe.FP_MXFP4, moqe.FP_NVFP4, moqe.FP_BF16):
+            assert L.moqe_fp_quantize(P, N, K, fmt, None, C.byref(out)) == moqe.ERR_UNSUPPORTED
+            assert L.moqe_fp_expert_import(N, K, fmt, P, P, None, P, None, C.byref(out)) == moqe.ERR_UNSUPPORTED
+    assert L.moqe_fp4_quantize_rows(P, 1, (1 << 24) + 8, moqe.FP_NVFP4, P, P, P, P, None) == moqe.ERR_UNSUPPORTED
+
+
 def test_product(L):
     none = (C.c_void_p * 2)(None, None)
     for f in (lambda *a: L.moqe_routed_fpgemm(P, P, *a), lambda *a: L.moqe_routed_fpgemm_sorted(P, P, P, *a)):

@@ -138,3 +138,58 @@ def test_random_routings_and_sizes():
         Y = moqe.moqe_routed_fpgemm(X, ids, [e for e, _ in ex])
         _check(Y, X, ids, [w for _, w in ex], formats)
     assert moqe.moqe_async_status() == moqe.OK
+
+
+@pytest.mark.parametrize("fmt", [MX, NV, BF])
+@pytest.mark.parametrize("M", [1, 40, 300])
+def test_far_scales(fmt, M):
+    """A power of two on the weights and one on the rows come out as their product, to the bit: nothing on the way leaves fp32's range
+    as long as neither the sums nor the outputs do.  (One row takes a kernel of its own.)"""
+    N, K = 4096, 1024
+    g = np.random.default_rng(M)
+    W, X = g.standard_normal((N, K)).astype(np.float32), g.standard_normal((M, K)).astype(np.float32)
+    ids = torch.zeros(M, dtype=torch.int32, device="cuda")
+    run = lambda w, x: moqe.moqe_routed_fpgemm(_bf16(x), ids, [moqe.moqe_fp_quantize(_dev(w), fmt)])
+    Y = run(W, X).double()
+    for a, b in ((100, -100), (-100, 100), (50, 40), (-30, -30)):
+        assert torch.equal(run(np.ldexp(W, a), np.ldexp(X, b)).double(), Y * 2.0 ** (a + b)), (a, b)
+    # sums of zeros under scales whose product is beyond fp32
+    W[:, ::2] = 0
+    X[:, 1::2] = 0
+    assert bool((run(np.ldexp(W, 100), np.ldexp(X, 100)) == 0).all())
+
+
+def test_an_imported_outer_scale_meets_small_rows():
+    """The channel's scale goes to the sum first: its product with a small row's alone would be below fp32's normal numbers."""
+    N, K = 256, 512
+    g = np.random.default_rng(9)
+    e0 = moqe.moqe_fp_quantize(_dev(g.standard_normal((N, K)).astype(np.float32)), NV)
+    codes, scales, _, _ = moqe.moqe_fp_expert_export(e0)
+    outer = (1 + g.random(N)).astype(np.float32)
+    X = g.standard_normal((200, K)).astype(np.float32)
+    for M in (1, 200):
+        ids = torch.zeros(M, dtype=torch.int32, device="cuda")
+        run = lambda a, b: moqe.moqe_routed_fpgemm(_bf16(np.ldexp(X[:M], b)), ids, [moqe.moqe_fp_expert_import(NV, codes, scales, _dev(np.ldexp(outer, a)))])
+        assert torch.equal(run(30, -114).double(), run(0, 0).double() * 2.0 ** -84)
+        assert torch.equal(run(-40, -60).double(), run(0, 0).double() * 2.0 ** -100)
+
+
+def test_products_beyond_the_schedule_are_refused():
+    """(before a pointer is looked at)"""
+    import ctypes as C
+    L, p = moqe.lib(), 0x10000
+    e = moqe.moqe_fp_quantize(torch.zeros(65536, 4096, device="cuda"), BF)
+    arr = (C.c_void_p * 1)(e.handle)
+    for M in (2 ** 31 - 1, 2 ** 30 + 1, 2 ** 24):
+        assert L.moqe_routed_fpgemm_workspace(M, arr, 1) == 0
+        assert L.moqe_routed_fpgemm(p, p, M, arr, 1, p, p, 2 ** 62, None) == moqe.ERR_UNSUPPORTED
+        assert L.moqe_routed_fpgemm_sorted(p, p, p, M, arr, 1, p, p, 2 ** 62, None) == moqe.ERR_UNSUPPORTED
+    assert L.moqe_routed_fpgemm_workspace(2 ** 20, arr, 1) > 0
+
+
+def test_a_workspace_for_many_rows_serves_fewer():
+    for formats in ([NV], [MX, BF], [NV] * 31 + [BF]):
+        for N in (128, 512, 11008):
+            ex = [moqe.moqe_fp_quantize(torch.zeros(N, 256, device="cuda"), f) for f in formats]
+            sizes = [moqe.moqe_routed_fpgemm_workspace(M, ex) for M in sorted([*range(1, 300), *range(300, 20000, 37), 9344, 9345, 9472, 9473])]
+            assert all(a <= b for a, b in zip(sizes, sizes[1:]))
