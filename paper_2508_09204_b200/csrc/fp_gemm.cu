@@ -35,7 +35,7 @@ constexpr int FP_BAND = 8;                       // token tiles that are gone th
 constexpr int FP_EPI_WARPS = 8;
 constexpr int FP_WEIGHTS_WARP = FP_EPI_WARPS, FP_MMA_WARP = FP_EPI_WARPS + 1, FP_TOKENS_WARP = FP_EPI_WARPS + 2;
 constexpr int FP_THREADS = 32 * (FP_EPI_WARPS + 3);
-constexpr int FP_MAX_STAGES = 12;
+constexpr int FP_MAX_STAGES = 8;
 constexpr int FP_RING_BYTES = 200 * 1024;
 constexpr int FP_BOX = 32 * 64;                  // 32 tokens x 32 channels of bf16, an epilogue warp's
 constexpr int FP_SMEM = FP_RING_BYTES + FP_EPI_WARPS * FP_BOX + 1024;
@@ -59,7 +59,7 @@ struct FpGemmParams {
     __nv_bfloat16* Y;
     int* status;
     int E, N, NT, TN;            // NT: tiles of 128 channels; TN: tokens of a tile
-    int stages, stage_bytes, b_off, sfb_off;
+    int sf;                      // bytes of a tile's scales in a stage: the most of the call's formats
     int split_cost, least_share;     // what splitting costs, and the least share of a worker, in k-blocks
 };
 
@@ -67,6 +67,7 @@ struct FpSched {
     // by place in the order of work: bf16 experts first, whose tiles are four times as deep, then the 4-bit ones
     int order[MOQE_MAX_EXPERTS], tile0[MOQE_MAX_EXPERTS + 1], unit0[MOQE_MAX_EXPERTS + 1], KB[MOQE_MAX_EXPERTS], cost[MOQE_MAX_EXPERTS], tts[MOQE_MAX_EXPERTS];
     int off[MOQE_MAX_EXPERTS + 1], pad0[MOQE_MAX_EXPERTS], blk0[MOQE_MAX_EXPERTS], rpt[MOQE_MAX_EXPERTS];      // by expert: rows, padded rows and blocks of scales before it, rows of a token tile
+    int stages, stage_bytes, sfb_off;       // of the ring, which the largest token tile of the call decides
     int W, NT, all_deep;         // workers (CTAs or pairs); channel tiles of a worker; tiles of bf16 experts
     int deep, light;             // tiles dealt out whole: of bf16 experts; of 4-bit ones, behind all of those
     int late, extra;             // workers from `late` on, who have a deep tile less, have `extra` rounds of light ones before the others
@@ -226,6 +227,7 @@ __device__ __forceinline__ bool mbar_wait_two(uint32_t bar0, uint32_t parity0, u
 // lane's branch, operands moved to the uniform datapath), so it holds nothing that can be worked out before it.  One SM's tiles
 // are small: two k-blocks to a turn there.  A pair multiplies 256 tokens in 512 cycles or more, and would rather have its stages back.
 // A wait that runs out is looked at after the piece: what is issued until then stays in bounds, and no later wait takes long.
+struct FpStages { int stages, bytes, b_off, sfb_off; };
 struct FpIssue {
     Ring ring, last;             // the next stage; the last one (issued before it)
     Ring behind;                 // the stage whose k-block had the next set of scales
@@ -259,13 +261,13 @@ __device__ __forceinline__ void issue_kblock(uint32_t d, uint32_t a, uint32_t b_
     }
 }
 template <int CG, int FORMAT>
-__device__ __forceinline__ void issue_piece(FpIssue& q, const FpGemmParams& p, uint32_t ring0, uint32_t bar_full, uint32_t bar_empty, uint32_t d,
+__device__ __forceinline__ void issue_piece(FpIssue& q, const FpGemmParams& p, const FpStages& st, uint32_t ring0, uint32_t bar_full, uint32_t bar_empty, uint32_t d,
                                             uint32_t sf0, int n, int kblocks, uint32_t accfull, volatile int* abort_flag) {
     constexpr uint32_t SET = (FORMAT == MOQE_FP_MXFP4 ? 2 : 4) * (CG == 2 ? 12 : 8);        // columns of a set
     // With as many sets as stages, a stage that has been filled again frees its set.  A pair has room for two of NVFP4's.
     constexpr bool SCARCE = CG == 2 && FORMAT == MOQE_FP_NVFP4;
     constexpr int TURN = CG == 2 ? 1 : 2;
-    const int sets = SCARCE ? 2 : p.stages;
+    const int sets = SCARCE ? 2 : st.stages;
     const uint32_t id0 = FORMAT == MOQE_FP_BF16 ? idesc_bf16<CG>(n) : idesc_fp4<CG>(n, FORMAT == MOQE_FP_MXFP4, 0);
     if (FORMAT != MOQE_FP_BF16 && q.format != FORMAT) {
         // sets of another size, or none for a while: everything before must have been multiplied
@@ -278,23 +280,23 @@ __device__ __forceinline__ void issue_piece(FpIssue& q, const FpGemmParams& p, u
     for (int k = 0; k < kblocks; k += TURN) {
         const Ring r0 = q.ring;
         Ring r1 = r0;
-        r1.advance(p.stages);
+        r1.advance(st.stages);
         const bool two = TURN == 2 && k + 1 < kblocks;
         const uint32_t full0 = bar_full + 8 * r0.stage, full1 = bar_full + 8 * r1.stage;
         if constexpr (SCARCE) {
             if (q.fresh > 0) --q.fresh;
-            else { q.ok &= mbar_wait_short(bar_empty + 8 * q.behind.stage, q.behind.phase, abort_flag, p.status); q.behind.advance(p.stages); }
+            else { q.ok &= mbar_wait_short(bar_empty + 8 * q.behind.stage, q.behind.phase, abort_flag, p.status); q.behind.advance(st.stages); }
         }
         q.ok &= two ? mbar_wait_two(full0, r0.phase, full1, r1.phase, abort_flag, p.status) : mbar_wait_short(full0, r0.phase, abort_flag, p.status);
         __syncwarp();
         tc_fence_after();
-        const uint32_t a0 = ring0 + r0.stage * p.stage_bytes, a1 = ring0 + r1.stage * p.stage_bytes;
+        const uint32_t a0 = ring0 + r0.stage * st.bytes, a1 = ring0 + r1.stage * st.bytes;
         const int set1 = q.set + 1 >= sets ? 0 : q.set + 1;
         if (elect_one()) {
-            issue_kblock<CG, FORMAT>(d, a0, p.b_off, p.sfb_off, sf0 + q.set * SET, id0, n, k == 0);
+            issue_kblock<CG, FORMAT>(d, a0, st.b_off, st.sfb_off, sf0 + q.set * SET, id0, n, k == 0);
             fp_commit<CG>(bar_empty + 8 * r0.stage);
             if (two) {
-                issue_kblock<CG, FORMAT>(d, a1, p.b_off, p.sfb_off, sf0 + set1 * SET, id0, n, false);
+                issue_kblock<CG, FORMAT>(d, a1, st.b_off, st.sfb_off, sf0 + set1 * SET, id0, n, false);
                 fp_commit<CG>(bar_empty + 8 * r1.stage);
             }
             if (k + TURN >= kblocks) fp_commit<CG>(accfull);
@@ -302,7 +304,7 @@ __device__ __forceinline__ void issue_piece(FpIssue& q, const FpGemmParams& p, u
         __syncwarp();
         q.last = two ? r1 : r0;
         q.ring = q.last;
-        q.ring.advance(p.stages);
+        q.ring.advance(st.stages);
         q.set = !two ? set1 : set1 + 1 == sets ? 0 : set1 + 1;
     }
 }
@@ -390,7 +392,7 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
 
     if (threadIdx.x == FP_WEIGHTS_WARP * 32) {
         // (weights and tokens arrive on their own; a pair's first CTA issues the MMAs: its full barriers take an arrival for the other CTA, too)
-        for (int i = 0; i < p.stages; ++i) { mbar_init(bar_full + 8 * i, CG == 2 && rank == 0 ? 3 : 2); mbar_init(bar_empty + 8 * i, 1); }
+        for (int i = 0; i < FP_MAX_STAGES; ++i) { mbar_init(bar_full + 8 * i, CG == 2 && rank == 0 ? 3 : 2); mbar_init(bar_empty + 8 * i, 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(bar_accfull + 8 * i, 1); mbar_init(bar_accempty + 8 * i, FP_EPI_WARPS * CG); }
         sh.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -403,7 +405,7 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
             const int lo = is ? __ldcg(p.offsets + lane) : 0, hi = is ? __ldcg(p.offsets + lane + 1) : 0;
             const uint32_t bf = __ballot_sync(0xFFFFFFFFu, deep), four = __ballot_sync(0xFFFFFFFFu, is && !deep), below = (1u << lane) - 1u;
             const TokenTiles t = token_tiles(hi - lo, p.TN);
-            const int pad = (hi - lo + 15) & ~15, blocks = t.tiles * (p.TN > 128 ? 2 : 1);
+            const int pad = (hi - lo + 15) & ~15, most = __reduce_max_sync(0xFFFFFFFFu, t.tiles > 1 ? t.rows : pad), blocks = t.tiles * (p.TN > 128 ? 2 : 1);
             int psum = pad, bsum = blocks;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
@@ -415,7 +417,16 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
                 sh.pad0[lane] = psum - pad;
                 sh.blk0[lane] = bsum - blocks;
                 sh.rpt[lane] = t.rows;
-                if (lane == p.E - 1) sh.off[p.E] = hi;
+                if (lane == p.E - 1) {
+                    sh.off[p.E] = hi;
+                    // A stage: weights, their scales, token rows (from a multiple of 1024), their scales; as many as fit, and as there is
+                    // room for sets of scales.  (Sized for 128 tokens where a call's largest tile has 48, 18944 channels x 3584 k of two
+                    // formats take 21.8 instead of 20.8 us; 512 rows of three, 4096 x 4096, 28.6 for 25.1.)
+                    const int at = 16384 + p.sf + most / CG * 128, bytes = (at + (most > 128 ? 2 : 1) * p.sf + 1023) & ~1023;
+                    sh.sfb_off = at;
+                    sh.stage_bytes = bytes;
+                    sh.stages = min(FP_RING_BYTES / bytes, CG == 2 && p.sf ? 5 : 8);
+                }
                 sh.order[deep ? __popc(bf & below) : __popc(bf) + __popc(four & below)] = lane;
             }
         }
@@ -480,6 +491,7 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
     }
     tc_fence_after();
     const uint32_t tmem = warp == FP_WEIGHTS_WARP ? 0u : sh.tmem;
+    const FpStages st = {sh.stages, sh.stage_bytes, 16384 + p.sf, sh.sfb_off};
 
     if (warp == FP_WEIGHTS_WARP) {
         // ---------------- weights and their scales ----------------
@@ -496,12 +508,12 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
                 for (int k = pc.kb1 - pc.kb0; k > 0; --k, src += stride) {
                     if (!(ok = mbar_wait_short(bar_empty + 8 * ring.stage, ring.phase ^ 1u, &sh.abort, p.status))) break;
                     mbar_expect_tx(bar_full + 8 * ring.stage, stride);
-                    bulk_load(ring0 + ring.stage * p.stage_bytes, src, stride, bar_full + 8 * ring.stage);
-                    ring.advance(p.stages);
+                    bulk_load(ring0 + ring.stage * st.bytes, src, stride, bar_full + 8 * ring.stage);
+                    ring.advance(st.stages);
                 }
             }
             // (the last stages are handed back by arrivals from the tensor cores, a pair's second CTA's from the first: they land here)
-            for (int i = 0; ok && i < p.stages; ++i, ring.advance(p.stages)) ok = mbar_wait_short(bar_empty + 8 * ring.stage, ring.phase ^ 1u, &sh.abort, p.status);
+            for (int i = 0; ok && i < st.stages; ++i, ring.advance(st.stages)) ok = mbar_wait_short(bar_empty + 8 * ring.stage, ring.phase ^ 1u, &sh.abort, p.status);
         }
         __syncwarp();
         if constexpr (CG == 2) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
@@ -524,11 +536,11 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
                 const uint8_t* ssrc = p.t.sf + sh.blk0[pc.e] * p.t.block_sf + pc.kb0 * sstep + (size_t)(pc.tt * bpt) * sfb;
                 for (int k = pc.kb1 - pc.kb0; k > 0; --k, src += step, ssrc += sstep) {
                     if (!(ok = mbar_wait_short(bar_empty + 8 * ring.stage, ring.phase ^ 1u, &sh.abort, p.status))) break;
-                    const uint32_t full = bar_full + 8 * ring.stage, base = ring0 + ring.stage * p.stage_bytes;
+                    const uint32_t full = bar_full + 8 * ring.stage, base = ring0 + ring.stage * st.bytes;
                     mbar_expect_tx(full, bytes + sbytes);
-                    bulk_load(base + p.b_off, src, bytes, full);
-                    if (sbytes) bulk_load(base + p.sfb_off, ssrc, sbytes, full);
-                    ring.advance(p.stages);
+                    bulk_load(base + st.b_off, src, bytes, full);
+                    if (sbytes) bulk_load(base + st.sfb_off, ssrc, sbytes, full);
+                    ring.advance(st.stages);
                 }
             }
         }
@@ -547,9 +559,9 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
             // one SM: the accumulator of two tiles ago has been read; a pair: what this one shares with the last has
             const uint32_t before = CG == 2 ? uses + 1 : uses, d = tmem + buf * L::ACC1, accfull = bar_accfull + 8 * buf;
             q.ok = mbar_wait_short(bar_accempty + 8 * (before & 1), ((before >> 1) & 1u) ^ 1u, &sh.abort, p.status);
-            if (format == MOQE_FP_MXFP4) issue_piece<CG, MOQE_FP_MXFP4>(q, p, ring0, bar_full, bar_empty, d, sf0, n, pc.kb1 - pc.kb0, accfull, &sh.abort);
-            else if (format == MOQE_FP_NVFP4) issue_piece<CG, MOQE_FP_NVFP4>(q, p, ring0, bar_full, bar_empty, d, sf0, n, pc.kb1 - pc.kb0, accfull, &sh.abort);
-            else issue_piece<CG, MOQE_FP_BF16>(q, p, ring0, bar_full, bar_empty, d, sf0, n, pc.kb1 - pc.kb0, accfull, &sh.abort);
+            if (format == MOQE_FP_MXFP4) issue_piece<CG, MOQE_FP_MXFP4>(q, p, st, ring0, bar_full, bar_empty, d, sf0, n, pc.kb1 - pc.kb0, accfull, &sh.abort);
+            else if (format == MOQE_FP_NVFP4) issue_piece<CG, MOQE_FP_NVFP4>(q, p, st, ring0, bar_full, bar_empty, d, sf0, n, pc.kb1 - pc.kb0, accfull, &sh.abort);
+            else issue_piece<CG, MOQE_FP_BF16>(q, p, st, ring0, bar_full, bar_empty, d, sf0, n, pc.kb1 - pc.kb0, accfull, &sh.abort);
             q.ok = __all_sync(0xFFFFFFFFu, q.ok);
             ++uses;
         }
@@ -566,7 +578,7 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
                 for (int kb = pc.kb0; kb < pc.kb1; ++kb) {
                     if (!(ok = mbar_wait_short(bar_full + 8 * ring.stage, ring.phase, &sh.abort, p.status))) break;
                     leader_arrive(to + 8 * ring.stage);
-                    ring.advance(p.stages);
+                    ring.advance(st.stages);
                 }
             }
         }
@@ -844,15 +856,8 @@ moqe_status launch_fp_gemm(const moqe_fp_expert* const* ex, int E, int M, const 
     const FpTile tile = pick_tile(M, ex, E);
     const bool pair = tile.pair;
     p.TN = tile.TN;
-    // a stage: weights, their scales, token rows (from a multiple of 1024), their scales
-    p.b_off = 16384 + sf;
-    p.sfb_off = p.b_off + (pair ? p.TN / 2 : p.TN) * 128;
-    p.stage_bytes = (p.sfb_off + (pair ? 2 * sf : sf) + 1023) & ~1023;
-    p.stages = FP_RING_BYTES / p.stage_bytes;
-    if (p.stages > FP_MAX_STAGES) p.stages = FP_MAX_STAGES;
-    // (one SM, NVFP4: eight sets of 32 columns behind two accumulators of 128)
-    if (!pair && p.stages > 8) p.stages = 8;
-    static_assert(FP_RING_BYTES / (16384 + 1024 + 16384 + 2048) <= 5, "a pair has room for five sets of 24 columns");
+    p.sf = sf;
+    static_assert(FP_RING_BYTES / (16384 + 1024) >= 8 && FP_MAX_STAGES >= 8, "the ring's stages");
     // One SM's sums are parked and added up in some 20 k-blocks' time, a pair's (four times as many) in 36.  With 6 and 18 instead:
     // 48 rows of NVFP4, 4096 -> 11008, 18.9 us for 12.5; 512 rows in three formats 32 for 28.5; 4160 rows of 3584 -> 18944 295 for 285;
     // 2048 rows of bf16 62 for 59.
