@@ -3,10 +3,11 @@
 // A 4-bit number is e2m1 (0, .5, 1, 1.5, 2, 3, 4, 6 and a sign bit); 32 (MXFP4) or 16 (NVFP4) consecutive k share a scale, a
 // power of two (E8M0) or an e4m3 number; an NVFP4 row has an fp32 scale of its own on top.  See moqe.h for the arithmetic.
 //
-// Every rounding here is that of an exact real quotient.  MXFP4 divides by a power of two.  NVFP4 divides by an e4m3 number: for
-// a source of bf16 a quotient that is not half way between two numbers is at least 2^-9 of its size away from there, for fp32
-// 2^-24 of its size, so that the correctly rounded fp32 quotient can meet a half way mark it should not meet with fp32 sources
-// only, and there the sign of the remainder decides (nv_quotient).
+// Every rounding here is that of an exact real quotient.  MXFP4 divides by a power of two.  NVFP4 divides by an e4m3 number.  For a
+// source of bf16 a quotient that is not half way between two numbers is at least 2^-9 of its size away from there: a product with a
+// reciprocal that is a little too large, cut to 12 bits, is the half way mark where the quotient is, and on the quotient's side of it
+// elsewhere.  For fp32 it is 2^-24 of its size away, so that the correctly rounded fp32 quotient can meet a half way mark that it should
+// not meet, and there the sign of the remainder decides (nv_quotient).
 //
 // Packed layout, the same for experts and for a call's token rows: k-blocks of 128 bytes a row (256 codes or 64 bf16), in which a
 // row's eight 16-byte chunks are permuted by the 128-byte swizzle (chunk c of row r at place c ^ (r & 7)), eight rows to 1024
@@ -144,8 +145,21 @@ __device__ __forceinline__ uint32_t encode16(const float (&x)[16], float amax, i
         byte = e4m3_byte(nv_quotient<false>(amax * inv, 6.0f, 1.0f / 6.0f));
         const float s = e4m3_value(byte);
         const float rs = byte ? rcp_approx(s) : 0.f;
+        if constexpr (FP32) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) q[i] = copysignf(nv_quotient<FP32>(fabsf(x[i]) * inv, s, rs), x[i]);
+            for (int i = 0; i < 16; ++i) q[i] = copysignf(nv_quotient<true>(fabsf(x[i]) * inv, s, rs), x[i]);
+        } else {
+            float k = rs * 0x1.000008p0f * inv;                 // (a factor of 1 + 2^-21)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) q[i] = x[i];
+            if (row_field < 32) {                               // (a row of tiny numbers, for which k could be infinite)
+                k = rs * 0x1.000008p0f * pow2_field(190 - row_field);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) q[i] *= 0x1p64f;
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) q[i] = __uint_as_float(__float_as_uint(q[i] * k) & 0xFFFFF000u);
+        }
     }
     codes[0] = e2m1_x8(q);
     codes[1] = e2m1_x8(q + 8);
@@ -204,9 +218,22 @@ __device__ __forceinline__ float amax16(const float (&x)[16]) {
     for (int i = 3; i < 15; i += 2) m = max_abs3(m, x[i], x[i + 1]);
     return max_abs3(m, x[15], x[15]);
 }
-__device__ __forceinline__ uint32_t finite_amax16(const float (&x)[16]) {
-    uint32_t m = __float_as_uint(amax16(x));
+// the same of 16 numbers as they were loaded
+__device__ __forceinline__ float raw_amax(const RawF32& raw) { float x[16]; widen(raw, x); return amax16(x); }
+__device__ __forceinline__ float raw_amax(const RawBf16& raw) {
+    uint32_t m = raw.r.w[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) asm("max.NaN.xorsign.abs.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(raw.r.w[i]));
+    const float lo = __uint_as_float(m << 16), hi = __uint_as_float(m & 0xFFFF0000u);
+    return max_abs3(lo, hi, hi);
+}
+// ... of those that are finite; a: of all
+template <class Raw>
+__device__ __forceinline__ uint32_t finite_amax(const Raw& raw, float a) {
+    uint32_t m = __float_as_uint(a);
     if (m >= 0x7F800000u) {
+        float x[16];
+        widen(raw, x);
         m = 0;
 #pragma unroll
         for (int i = 0; i < 16; ++i) { const uint32_t b = __float_as_uint(x[i]) & 0x7FFFFFFFu; m = max(m, b < 0x7F800000u ? b : 0u); }
@@ -232,6 +259,7 @@ __device__ __forceinline__ void encode_row(const T* row, int have, int padded, b
     constexpr bool FP32 = sizeof(T) == 4;
     const int span = nt * 16 * CHUNKS, parts = (padded + span - 1) / span, k0 = tid * 16, step = nt * 16;
     typename RawOf<T>::type raw[CHUNKS];
+    float most[CHUNKS];
     int field = 127;
     if constexpr (FORMAT == MOQE_FP_NVFP4) {
         uint32_t m = 0;
@@ -239,7 +267,7 @@ __device__ __forceinline__ void encode_row(const T* row, int have, int padded, b
 #pragma unroll
             for (int i = 0; i < CHUNKS; ++i) load16(row, part * span + k0 + i * step, have, wide, raw[i]);
 #pragma unroll
-            for (int i = 0; i < CHUNKS; ++i) { float x[16]; widen(raw[i], x); m = max(m, finite_amax16(x)); }
+            for (int i = 0; i < CHUNKS; ++i) { most[i] = raw_amax(raw[i]); m = max(m, finite_amax(raw[i], most[i])); }
         }
         field = nv_row_field(nt == 32 ? __reduce_max_sync(0xFFFFFFFFu, m) : block_max(m, buf));
         if (outer && tid == 0) *outer = pow2_field(field);
@@ -255,7 +283,7 @@ __device__ __forceinline__ void encode_row(const T* row, int have, int padded, b
             if (k - (int)(threadIdx.x & 31) * 16 >= padded) break;         // (the whole warp)
             float x[16];
             widen(raw[i], x);
-            float a = amax16(x);
+            float a = FORMAT == MOQE_FP_NVFP4 ? parts > 1 ? raw_amax(raw[i]) : most[i] : amax16(x);
             uint32_t codes[2];
             if constexpr (FORMAT == MOQE_FP_MXFP4) { const float b = __shfl_xor_sync(0xFFFFFFFFu, a, 1); a = max_abs3(a, b, b); }
             const uint32_t byte = encode16<FORMAT, FP32>(x, a, field, codes);

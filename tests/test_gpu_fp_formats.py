@@ -170,3 +170,21 @@ def test_refusals_of_the_binding():
                                    scales=torch.zeros(8, 3, dtype=torch.uint8, device="cuda"))
     with pytest.raises(moqe.MoqeError):
         moqe.moqe_fp_expert_import(moqe.FP_BF16)
+
+
+@pytest.mark.parametrize("power", [0, -60, -125, 90])
+def test_every_tie_under_every_scale(power):
+    """NVFP4: each block's largest number makes its scale, the others are its half way marks and their bf16 neighbours on both sides."""
+    marks = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0])
+    rows = []
+    for b in range(1, 127):
+        s = (b & 7) * 2.0 ** -9 if b < 8 else (1 + (b & 7) / 8) * 2.0 ** ((b >> 3) - 7)
+        if 6 * s >= 2048:
+            continue
+        ties = (marks * s).astype(np.float32).view(np.uint32)
+        assert np.array_equal(ties & 0xFFFF, 0 * ties)                       # (seven bits: bf16 has them)
+        for step in (-0x10000, 0, 0x10000):
+            near = (ties.astype(np.int64) + step).astype(np.uint32).view(np.float32)
+            rows.append(np.concatenate([[6 * s], near, -near, [0], [1536], 15 * [0]]))    # the row's scale is 1
+    X = torch.from_numpy(np.ldexp(np.array(rows, dtype=np.float32), power)).to(torch.bfloat16).cuda()
+    _check(*moqe.moqe_fp4_quantize_rows(X, moqe.FP_NVFP4, values=True), R.encode(X.float().cpu().numpy(), moqe.FP_NVFP4))
