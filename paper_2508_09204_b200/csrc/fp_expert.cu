@@ -28,7 +28,9 @@ __global__ void __maxnreg__(64) fp_build_kernel(const float* __restrict__ W, int
                     make_uint4(pack_bf16x2(x[8 * h], x[8 * h + 1]), pack_bf16x2(x[8 * h + 2], x[8 * h + 3]), pack_bf16x2(x[8 * h + 4], x[8 * h + 5]), pack_bf16x2(x[8 * h + 6], x[8 * h + 7]));
         }
     } else {
-        encode_row<FORMAT, 2>(row, have, padded, wide, at.tid, at.nt, buf, outer ? outer + n : nullptr, [&](int k, uint32_t byte, const uint32_t (&c)[2], int) { put_packed<FORMAT>(out, k, padded, byte, c); });
+        const PackedLane to = packed_lane<FORMAT>(out, at.tid, at.nt);
+        encode_row<FORMAT, 2>(row, have, padded, wide, at.tid, at.nt, buf, outer ? outer + n : nullptr,
+                              [&](int k, int chunk, uint32_t byte, const uint32_t (&c)[2], int) { put_packed<FORMAT>(to, chunk, k < padded, byte, c); });
     }
 }
 

@@ -59,9 +59,16 @@ __host__ __device__ inline TokenTiles token_tiles(int n, int TN) {
     const int t = (n + TN - 1) / TN;
     return {t, t > 1 ? ((n + t - 1) / t + 15) & ~15 : TN};
 }
+// a / b for 0 <= a, 0 < b (a 32-bit division takes far longer; the quotient is a few units off at most)
+__device__ __forceinline__ int div_small(int a, int b) {
+    int q = (int)((float)a * __frcp_rz((float)b));
+    while ((q + 1) * b <= a) ++q;
+    while (q * b > a) --q;
+    return q;
+}
 // row i of a segment of `pad` rows; scales in blocks of 128 rows, as many to a tile as TN tokens need
 __device__ __forceinline__ PackedRow token_row(uint8_t* codes, uint8_t* sf, int format, int i, int pad, const TokenTiles& t, int TN) {
-    const int sfb = fp_sf_bytes(format), bpt = TN > 128 ? 2 : 1, tile = t.tiles > 1 ? i / t.rows : 0, in = i - tile * t.rows, r = in & 127;
+    const int sfb = fp_sf_bytes(format), bpt = TN > 128 ? 2 : 1, tile = t.tiles > 1 ? div_small(i, t.rows) : 0, in = i - tile * t.rows, r = in & 127;
     return {codes + (size_t)(i >> 3) * 1024 + (i & 7) * 128, (size_t)pad * 128,
             sf + (size_t)(tile * bpt + (in >> 7)) * sfb + (r & 31) * 16 + (r >> 5) * 4, (size_t)(t.tiles * bpt) * sfb, i & 7};
 }
@@ -69,8 +76,9 @@ __device__ __forceinline__ PackedRow token_row(uint8_t* codes, uint8_t* sf, int 
 __device__ __forceinline__ float pow2_field(int field) { return __int_as_float(field << 23); }   // 2^(field - 127), 1 <= field <= 254
 __device__ __forceinline__ float e8m0_value(uint32_t b) { return b == 0 ? __int_as_float(0x00400000) : b == 255 ? __int_as_float(0x7FC00000) : pow2_field((int)b); }
 __device__ __forceinline__ float e4m3_value(uint32_t b) {       // 0 <= b <= 127
-    if (b == 127) return __int_as_float(0x7FC00000);
-    return b < 8 ? (float)b * 0x1p-9f : __int_as_float((int)((b << 20) + (120u << 23)));
+    uint32_t h;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)b));
+    return __low2float(*reinterpret_cast<const __half2*>(&h));
 }
 
 // eight e2m1 codes, the first in the lowest nibble; to nearest, ties to the even code, beyond 6 to 6
@@ -220,12 +228,14 @@ __device__ __forceinline__ float amax16(const float (&x)[16]) {
 }
 // the same of 16 numbers as they were loaded
 __device__ __forceinline__ float raw_amax(const RawF32& raw) { float x[16]; widen(raw, x); return amax16(x); }
+// (magnitudes of pairs; the signs that come out are of no use)
+__device__ __forceinline__ uint32_t max_abs_bf16x2(uint32_t a, uint32_t b) { uint32_t d; asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b)); return d; }
+__device__ __forceinline__ float larger_half(uint32_t two) { const float lo = __uint_as_float(two << 16), hi = __uint_as_float(two & 0xFFFF0000u); return max_abs3(lo, hi, hi); }
 __device__ __forceinline__ float raw_amax(const RawBf16& raw) {
     uint32_t m = raw.r.w[0];
 #pragma unroll
-    for (int i = 1; i < 8; ++i) asm("max.NaN.xorsign.abs.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(raw.r.w[i]));
-    const float lo = __uint_as_float(m << 16), hi = __uint_as_float(m & 0xFFFF0000u);
-    return max_abs3(lo, hi, hi);
+    for (int i = 1; i < 8; ++i) m = max_abs_bf16x2(m, raw.r.w[i]);
+    return larger_half(m);
 }
 // ... of those that are finite; a: of all
 template <class Raw>
@@ -250,7 +260,7 @@ __device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t* buf) {
 }
 
 // One row by `nt` threads, a whole block or one of its warps (then `tid` is the lane): every chunk of the `padded` k is encoded and
-// handed to `sink(k, byte, codes, field)` by all lanes of its warp together; NVFP4's row scale comes first (from registers where the row fits into them, else the row is read twice).
+// handed to `sink(k, chunk, byte, codes, field)`, `chunk` its number among the thread's, by all lanes of its warp together; NVFP4's row scale comes first (from registers where the row fits into them, else the row is read twice).
 // `wide`: rows begin on 32-byte boundaries.
 template <class T> struct RawOf { typedef RawBf16 type; };
 template <> struct RawOf<float> { typedef RawF32 type; };
@@ -287,7 +297,7 @@ __device__ __forceinline__ void encode_row(const T* row, int have, int padded, b
             uint32_t codes[2];
             if constexpr (FORMAT == MOQE_FP_MXFP4) { const float b = __shfl_xor_sync(0xFFFFFFFFu, a, 1); a = max_abs3(a, b, b); }
             const uint32_t byte = encode16<FORMAT, FP32>(x, a, field, codes);
-            sink(k, byte, codes, field);
+            sink(k, part * CHUNKS + i, byte, codes, field);
         }
     }
 }
@@ -308,18 +318,22 @@ __device__ __forceinline__ RowPlace row_place(bool warps) {
     if (warps) return {(int)(blockIdx.x * ROWS_OF_WARPS + (threadIdx.x >> 5)), (int)(threadIdx.x & 31), 32};
     return {(int)blockIdx.x, (int)threadIdx.x, (int)blockDim.x};
 }
-// ... into a packed row: four scales to a store.  (All lanes of a warp; `padded` is a multiple of 256, so half warps are there as a whole.)
+// ... into a packed row, of which a thread has every nt-th chunk, the same place in some k-blocks: four scales to a store.  (All lanes of
+// a warp; `padded` is a multiple of 256, so half warps are there as a whole.)
+struct PackedLane { uint8_t *code, *scale; size_t code_step, scale_step; };
 template <int FORMAT>
-__device__ __forceinline__ void put_packed(const PackedRow& out, int k, int padded, uint32_t byte, const uint32_t (&codes)[2]) {
+__device__ __forceinline__ PackedLane packed_lane(const PackedRow& out, int tid, int nt) {
+    const int kb = tid >> 4, in = tid & 15;                               // (nt is a multiple of 32)
+    return {out.chunk(kb, in >> 1) + (in & 1) * 8, out.scale(kb, FORMAT == MOQE_FP_MXFP4 ? in >> 1 : in), (nt >> 4) * out.codes_kb, (nt >> 4) * out.sf_kb};
+}
+template <int FORMAT>
+__device__ __forceinline__ void put_packed(const PackedLane& out, int chunk, bool inside, uint32_t byte, const uint32_t (&codes)[2]) {
     constexpr int LANES = FORMAT == MOQE_FP_MXFP4 ? 2 : 1;                 // of a block
-    const int kb = k >> 8, in = k & 255;
-    uint32_t w = byte;
-    w |= __shfl_down_sync(0xFFFFFFFFu, byte, LANES) << 8;
-    w |= __shfl_down_sync(0xFFFFFFFFu, byte, 2 * LANES) << 16;
-    w |= __shfl_down_sync(0xFFFFFFFFu, byte, 3 * LANES) << 24;
-    if (k >= padded) return;
-    *reinterpret_cast<uint2*>(out.chunk(kb, in >> 5) + ((in >> 1) & 8)) = make_uint2(codes[0], codes[1]);
-    if ((threadIdx.x & (4 * LANES - 1)) == 0) *reinterpret_cast<uint32_t*>(out.scale(kb, in / (16 * LANES))) = w;
+    uint32_t w = byte | __shfl_down_sync(0xFFFFFFFFu, byte, LANES) << 8;
+    w |= __shfl_down_sync(0xFFFFFFFFu, w, 2 * LANES) << 16;
+    if (!inside) return;
+    *reinterpret_cast<uint2*>(out.code + chunk * out.code_step) = make_uint2(codes[0], codes[1]);
+    if ((threadIdx.x & (4 * LANES - 1)) == 0) *reinterpret_cast<uint32_t*>(out.scale + chunk * out.scale_step) = w;
 }
 
 // quantize.cu: device memory of experts (a pool of the library's)

@@ -82,13 +82,6 @@ struct FpSched {
 // k-blocks [kb0, kb1) of channel tile nt of the tokens [i0, i0 + rows) of expert e; at: its place in the order; tile: the expert's
 struct FpPiece { int e, nt, tt, i0, rows, kb0, kb1, KB, at, tile; };
 
-// a / b for 0 <= a, 0 < b (a 32-bit division takes far longer; the quotient is a few units off at most)
-__device__ __forceinline__ int div_small(int a, int b) {
-    int q = (int)((float)a * __frcp_rz((float)b));
-    while ((q + 1) * b <= a) ++q;
-    while (q * b > a) --q;
-    return q;
-}
 // tokens [i0, i0 + rows) and channel tile of an expert's tile: bands of FP_BAND token tiles, in a band channel tile by channel tile
 __device__ __forceinline__ void place_tile(const FpSched& s, FpPiece& pc) {
     const int band = div_small(pc.tile, FP_BAND * s.NT), in = pc.tile - band * FP_BAND * s.NT, deep = min(FP_BAND, s.tts[pc.at] - band * FP_BAND);

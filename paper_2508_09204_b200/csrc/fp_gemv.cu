@@ -131,7 +131,7 @@ __device__ __forceinline__ void gemv(const GemvParams& p, const GemvExpert& x, i
             reinterpret_cast<uint4*>(smem)[c] = c * 8 < p.K ? *reinterpret_cast<const uint4*>(row + c * 8) : make_uint4(0, 0, 0, 0);
     } else {
         int f = 127;
-        encode_row<FORMAT, 3>(row, p.K, x.KB * 256, p.wide, (int)threadIdx.x, (int)blockDim.x, buf, nullptr, [&](int k, uint32_t byte, const uint32_t (&c)[2], int field) {
+        encode_row<FORMAT, 3>(row, p.K, x.KB * 256, p.wide, (int)threadIdx.x, (int)blockDim.x, buf, nullptr, [&](int k, int, uint32_t byte, const uint32_t (&c)[2], int field) {
             f = field;
             if (k >= x.KB * 256) return;
             uint32_t o[4];

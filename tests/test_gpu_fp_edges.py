@@ -193,3 +193,30 @@ def test_a_workspace_for_many_rows_serves_fewer():
             ex = [moqe.moqe_fp_quantize(torch.zeros(N, 256, device="cuda"), f) for f in formats]
             sizes = [moqe.moqe_routed_fpgemm_workspace(M, ex) for M in sorted([*range(1, 300), *range(300, 20000, 37), 9344, 9345, 9472, 9473])]
             assert all(a <= b for a, b in zip(sizes, sizes[1:]))
+
+
+@pytest.mark.parametrize("M,K", [(1100, 8200), (300, 32768), (300, 32776), (20000, 456), (9100, 1000)])
+def test_many_rows_with_infinities_and_rows_of_nobody(M, K):
+    """Rows that a ring in shared memory takes, on both sides of its limits: every format in turn, blocks that are NaN, zeros."""
+    N, formats = 136, [NV, MX, BF, NV]
+    g = np.random.default_rng(M)
+    ex = [_expert(e, N, K, f) for e, f in enumerate(formats)]
+    x = g.standard_normal((M, K)).astype(np.float32)
+    x[5::97] = 0
+    x[7::101] *= 1e-38
+    X = _bf16(x)
+    ids = _dev(g.integers(-1, 5, M).astype(np.int32))
+    handles = [e for e, _ in ex]
+    Y = moqe.moqe_routed_fpgemm(X, ids, handles)
+    moqe.moqe_async_status()
+    _check(Y, X, ids, [w for _, w in ex], formats)
+    bad = torch.arange(3, M, 50, device="cuda")
+    X[bad, torch.randint(0, K, bad.shape, device="cuda", generator=torch.Generator("cuda").manual_seed(1))] = float("inf")
+    Z = moqe.moqe_routed_fpgemm(X, ids, handles)
+    moqe.moqe_async_status()
+    good = torch.ones(M, dtype=torch.bool, device="cuda")
+    good[bad] = False
+    assert torch.equal(Z[good], Y[good])
+    hit = bad[(ids[bad] >= 0) & (ids[bad] < 4)]
+    four = hit[ids[hit] != 2]
+    assert bool(Z[four].isnan().all()) and not bool(Z[hit].isfinite().any())
