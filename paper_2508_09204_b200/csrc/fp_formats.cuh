@@ -52,19 +52,20 @@ __device__ __forceinline__ PackedRow expert_row(uint8_t* tiles, int KB, int form
     uint8_t* t = tiles + (size_t)(n >> 7) * KB * stride;
     return {t + (r >> 3) * 1024 + (r & 7) * 128, (size_t)stride, t + 16384 + (r & 31) * 16 + (r >> 5) * 4, (size_t)stride, r & 7};
 }
-// The token tiles of an expert's n rows: as few as TN tokens allow, of equal size (a multiple of 16), because a tile of 16 tokens costs
-// two thirds of one of 256.
-struct TokenTiles { int tiles, rows; };
-__host__ __device__ inline TokenTiles token_tiles(int n, int TN) {
-    const int t = (n + TN - 1) / TN;
-    return {t, t > 1 ? ((n + t - 1) / t + 15) & ~15 : TN};
-}
+__device__ __forceinline__ float rcp_approx(float s) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s)); return r; }
 // a / b for 0 <= a, 0 < b (a 32-bit division takes far longer; the quotient is a few units off at most)
 __device__ __forceinline__ int div_small(int a, int b) {
-    int q = (int)((float)a * __frcp_rz((float)b));
+    int q = (int)((float)a * rcp_approx((float)b));
     while ((q + 1) * b <= a) ++q;
     while (q * b > a) --q;
     return q;
+}
+// The token tiles of an expert's n rows: as few as TN tokens allow, of equal size (a multiple of 16), because a tile of 16 tokens costs
+// two thirds of one of 256.
+struct TokenTiles { int tiles, rows; };
+__device__ __forceinline__ TokenTiles token_tiles(int n, int TN) {
+    const int t = (n + TN - 1) >> (31 - __clz(TN));       // (TN: a power of two)
+    return {t, t > 1 ? (div_small(n + t - 1, t) + 15) & ~15 : TN};
 }
 // row i of a segment of `pad` rows; scales in blocks of 128 rows, as many to a tile as TN tokens need
 __device__ __forceinline__ PackedRow token_row(uint8_t* codes, uint8_t* sf, int format, int i, int pad, const TokenTiles& t, int TN) {
@@ -130,7 +131,6 @@ __device__ __forceinline__ float nv_quotient(float y, float s, float rs) {
     }
     return q;
 }
-__device__ __forceinline__ float rcp_approx(float s) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s)); return r; }
 
 // Scale and codes of 16 consecutive k of a row.  `amax`: the largest magnitude of the numbers that share the scale (a NaN if there is
 // one among them); `row_field`: NVFP4's row scale is 2^(row_field - 127).  -> the scale's byte; the codes, the first in the lowest nibble.

@@ -76,7 +76,7 @@ struct FpSched {
     int abort;
     // Where worker w's share begins (u0 and the end of everything for w = 0 and G): a k-block belongs to the share that its start
     // is in.
-    __device__ __forceinline__ int cut(int w) const { return u0 + w * q + (int)((unsigned)(w * r) / (unsigned)G) + max(0, w - late) * more; }
+    __device__ __forceinline__ int cut(int w) const { return u0 + w * q + div_small(w * r, G) + max(0, w - late) * more; }
 };
 
 // k-blocks [kb0, kb1) of channel tile nt of the tokens [i0, i0 + rows) of expert e; at: its place in the order; tile: the expert's
@@ -445,31 +445,31 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
             // 74 workers: 303 us, 369 with shares of all but two rounds of 4-bit tiles).
             const bool is_deep = is && p.ex[e].format == MOQE_FP_BF16;
             const int T = __shfl_sync(0xFFFFFFFFu, tsum, 31), U = __shfl_sync(0xFFFFFFFFu, usum, 31), W = (int)gridDim.x / CG;
-            const int Tb = __reduce_add_sync(0xFFFFFFFFu, is_deep ? tiles : 0), Tl = T - Tb, rb = Tb / W, b = Tb - rb * W;
+            const int Tb = __reduce_add_sync(0xFFFFFFFFu, is_deep ? tiles : 0), Tl = T - Tb, rb = div_small(Tb, W), b = Tb - rb * W, even = div_small(U, W);
             const int cb = __reduce_max_sync(0xFFFFFFFFu, is_deep && tiles ? KB * cost : 0), cl = __reduce_max_sync(0xFFFFFFFFu, is && !is_deep && tiles ? KB * cost : 0);
             const int split = p.split_cost * FP_COST_BF16;
             // all whole, `lane` rounds of light tiles for everybody: how many more for those without the last deep one, and how long it takes
-            const int few = b ? (rb + 1) * cb : 0, short_of = max(0, Tl - lane * W), rounds = (short_of + W - b - 1) / (W - b);
+            const int few = b ? (rb + 1) * cb : 0, short_of = max(0, Tl - lane * W), rounds = div_small(short_of + W - b - 1, W - b);
             const int takes = max(few + (b ? lane * cl : 0), rb * cb + (lane + rounds) * cl);
             const int best = __reduce_min_sync(0xFFFFFFFFu, takes), who = __ffs(__ballot_sync(0xFFFFFFFFu, takes == best)) - 1;
             const int extra_best = __shfl_sync(0xFFFFFFFFu, rounds, who);
             if (lane == 0) {
                 int whole = 0, extra = 0, late = 0, more = 0, R = U, G;
-                if (T > 0 && best <= U / W + split) { whole = T; extra = extra_best; late = b; R = 0; }
-                for (int n = T / W; whole == 0 && n > 0; --n) {
+                if (T > 0 && best <= even + split) { whole = T; extra = extra_best; late = b; R = 0; }
+                for (int n = div_small(T, W); whole == 0 && n > 0; --n) {
                     const int deep = min(Tb, n * W), rest = U - deep * cb - (n * W - deep) * cl;
                     const bool uneven = deep < n * W && b > 0;                  // workers from b on have had a deep tile less
                     const int d = uneven ? cb - cl : 0;
                     if (rest >= W * (cl ? cl : cb) && rest - (W - b) * d >= W * 4 * FP_COST_4BIT) { whole = n * W; R = rest; late = uneven ? b : 0; extra = uneven; more = d; }
                 }
-                G = whole ? W : max(max(1, min(T, W)), min(W, R / (p.least_share * FP_COST_BF16)));
+                G = whole ? W : max(max(1, min(T, W)), min(W, div_small(R, p.least_share * FP_COST_BF16)));
                 // few tiles, all alike: the same number of workers for each, so that nobody has the ends of two, if that is not much longer
-                if (whole == 0 && T > 0 && (Tb == 0 || Tb == T) && T <= G && max(cb, cl) / (G / T) <= R / G + split) G = G / T * T;
+                if (whole == 0 && T > 0 && (Tb == 0 || Tb == T) && T <= G && div_small(max(cb, cl), div_small(G, T)) <= div_small(R, G) + split) G = div_small(G, T) * T;
                 if (R == 0) G = 0;
                 sh.W = W; sh.NT = NT; sh.all_deep = Tb; sh.deep = min(Tb, whole); sh.light = whole - sh.deep; sh.late = late; sh.extra = extra; sh.more = more;
                 sh.u0 = sh.deep * cb + sh.light * cl; sh.G = G;
                 R -= max(0, G - late) * more;
-                sh.q = G ? R / G : 0; sh.r = G ? R - sh.q * G : 0;
+                sh.q = G ? div_small(R, G) : 0; sh.r = G ? R - sh.q * G : 0;
             }
         }
     }
@@ -516,11 +516,11 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
             FpWalk walk;
             FpPiece pc;
             Ring ring;
-            bool ok = true;
+            walk.start(sh, worker);
+            bool ok = walk.next(sh, p, pc);
             asm volatile("griddepcontrol.wait;" ::: "memory");
             asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-            walk.start(sh, worker);
-            while (ok && walk.next(sh, p, pc)) {
+            for (; ok; ok = ok && walk.next(sh, p, pc)) {
                 const int sfb = fp_sf_bytes(p.ex[pc.e].format), n = (pc.rows + 15) & ~15, bpt = p.TN > 128 ? 2 : 1;
                 const size_t pad0 = sh.pad0[pc.e], seg = (sh.off[pc.e + 1] - sh.off[pc.e] + 15) & ~15;
                 const uint32_t bytes = n / CG * 128, sbytes = n > 128 ? 2 * sfb : sfb;
