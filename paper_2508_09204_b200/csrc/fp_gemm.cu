@@ -11,7 +11,7 @@
 // One CTA to an SM; a worker is a CTA or a pair.  Two warps (one lane each) fill a ring of stages with bulk copies: weights with their
 // scales (one copy), which do not wait for the kernel that quantizes the rows; token rows and their scales (two).  One warp (one elected
 // lane) copies scales to tensor memory and issues the MMAs into one of two accumulators; eight warps read the other one, 32 channels
-// x 64 tokens each at a time, scale, round, turn them round with matrix stores and write 64 bytes a token.  Work: whole tiles
+// x twice 32 tokens each at a time, scale, round, turn them round with matrix stores and write 64 bytes a token.  Work: whole tiles
 // dealt out in turn where there are plenty; else, and for what is left over, the tiles' k-blocks in one sequence, an equal share to
 // every worker.  A warp that holds part of a tile parks its fp32 sums and counts itself in; the last one adds them up in the
 // order of the workers, so that a call gives the same bits every time.  Nobody waits for another worker.
@@ -577,7 +577,7 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
         }
         __syncwarp();
     } else {
-        // ---------------- epilogue: two warps to a quarter of the channels (TMEM lanes), 64 tokens each at a time ----------------
+        // ---------------- epilogue: two warps to a quarter of the channels (TMEM lanes), every other 32 tokens each ----------------
         asm volatile("griddepcontrol.wait;" ::: "memory");
         const int quarter = warp & 3, half = warp >> 2;
         const uint32_t box = ring0 + FP_RING_BYTES + warp * FP_BOX;
@@ -603,7 +603,7 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
             for (int g = 0; g < CG; ++g)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const int c = g * 128 + half * 64 + h * 32 + lane;
+                    const int c = g * 128 + h * 64 + half * 32 + lane;
                     to[g][h] = c < pc.rows ? p.perm[j0 + c] : 0;
                     sx[g][h] = ow && c < pc.rows ? ox[c] : 1.f;
                 }
@@ -619,10 +619,10 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
             for (int g = 0; g < CG; ++g) {
                 // a pair's first turn: the half that the accumulators share, columns 128.. of the first, 0.. of the second
                 const bool upper = CG == 2 && (g ^ buf ^ 1);
-                const int c = (upper ? 128 : 0) + half * 64, cols = pc.rows - c;
+                const int c = (upper ? 128 : 0) + half * 32, cols = pc.rows - c;        // 32 tokens, and 32 more 64 on
                 uint32_t v[64];
                 if (cols > 0) { tmem_ld_16x256(acc + c, v); tmem_ld_16x256(acc + (16u << 16) + c, v + 16); }
-                if (cols > 32) { tmem_ld_16x256(acc + c + 32, v + 32); tmem_ld_16x256(acc + (16u << 16) + c + 32, v + 48); }
+                if (cols > 64) { tmem_ld_16x256(acc + c + 64, v + 32); tmem_ld_16x256(acc + (16u << 16) + c + 64, v + 48); }
                 tmem_ld_wait();
                 if (g == 0) {
                     tc_fence_before();
@@ -634,15 +634,15 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
                         pack_block(v, ow != nullptr, w, upper ? sx[CG - 1][0] : sx[0][0], lane, o);
                         store_block(p, o, box, upper ? to[CG - 1][0] : to[0][0], cols, n0, lane);
                     }
-                    if (cols > 32) {
+                    if (cols > 64) {
                         pack_block(v + 32, ow != nullptr, w, upper ? sx[CG - 1][1] : sx[0][1], lane, o);
-                        store_block(p, o, box, upper ? to[CG - 1][1] : to[0][1], cols - 32, n0, lane);
+                        store_block(p, o, box, upper ? to[CG - 1][1] : to[0][1], cols - 64, n0, lane);
                     }
                 } else {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {           // (token block i / 2, channel half i % 2)
-                        const int r = 32 * (i >> 3) + 16 * (i & 1) + 4 * ((i >> 1) & 3);
-                        if (8 * (i >> 1) < cols) __stcg(slot + (c >> 3) * 256 + i * 128, make_uint4(v[r], v[r + 1], v[r + 2], v[r + 3]));
+                        const int r = 32 * (i >> 3) + 16 * (i & 1) + 4 * ((i >> 1) & 3), at = 8 * ((i >> 1) & 3) + 64 * (i >> 3);
+                        if (at < cols) __stcg(slot + ((c + at) >> 3) * 256 + (i & 1) * 128, make_uint4(v[r], v[r + 1], v[r + 2], v[r + 3]));
                     }
                 }
             }
@@ -683,7 +683,7 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
             for (int i = 0; i < 4; ++i) { const int n = n0 + (lane >> 2) + 8 * i; w[i] = ow && n < p.N ? ow[n] : 1.f; }
 #pragma unroll 1
             for (int g = 0; g < 2 * CG; ++g) {
-                const int c = (g >> 1) * 128 + half * 64 + (g & 1) * 32, cols = pc.rows - c;
+                const int c = (g >> 1) * 128 + half * 32 + (g & 1) * 64, cols = pc.rows - c;
                 if (cols <= 0) continue;
                 const int to = lane < cols ? p.perm[j0 + c + lane] : 0;
                 const float x = ow && lane < cols ? ox[c + lane] : 1.f;
