@@ -16,9 +16,9 @@
 // every worker.  A warp that holds part of a tile parks its fp32 sums and counts itself in; the last one adds them up in the
 // order of the workers, so that a call gives the same bits every time.  Nobody waits for another worker.
 //
-// Bound by HBM up to some 100 rows an expert (16 rows, 4096 -> 11008, three formats: 139.9 MB in 28.3 us with the kernel before it,
-// 76 % of the copy rate), by the tensor cores beyond (8192 x 4096 x 4096: bf16 178 us, 1540 TFLOP/s; MXFP4 59.7 us, 4600; NVFP4 67.6 us,
-// 4070).  A 4-bit k-block of a pair takes 512 cycles at the least; a turn of the issuing warp is about as long with NVFP4 (12
+// Bound by HBM up to some 100 rows an expert (16 rows, 4096 -> 11008, three formats: 139.9 MB in 27.2 us with the kernel before it,
+// 79 % of the copy rate), by the tensor cores beyond (8192 x 4096 x 4096: bf16 180 us, 1527 TFLOP/s; MXFP4 60.5 us, 4540; NVFP4 65.1 us,
+// 4220).  A 4-bit k-block of a pair takes 512 cycles at the least; a turn of the issuing warp is about as long with NVFP4 (12
 // copies of scales and 4 MMAs: 580 cycles), and the first k-blocks of a tile wait until half of the last accumulator has been read (1600
 // of a tile's 9800 cycles at k = 4096).
 //
