@@ -25,7 +25,7 @@ __global__ void __maxnreg__(64) fp_build_kernel(const float* __restrict__ W, int
 #pragma unroll
             for (int h = 0; h < 2; ++h)
                 *reinterpret_cast<uint4*>(out.chunk(k >> 6, ((k >> 3) & 7) + h)) =
-                    make_uint4(pack_bf16x2(x[8 * h], x[8 * h + 1]), pack_bf16x2(x[8 * h + 2], x[8 * h + 3]), pack_bf16x2(x[8 * h + 4], x[8 * h + 5]), pack_bf16x2(x[8 * h + 6], x[8 * h + 7]));
+                    make_uint4(bf16_pair(x[8 * h], x[8 * h + 1]), bf16_pair(x[8 * h + 2], x[8 * h + 3]), bf16_pair(x[8 * h + 4], x[8 * h + 5]), bf16_pair(x[8 * h + 6], x[8 * h + 7]));
         }
     } else {
         const PackedLane to = packed_lane<FORMAT>(out, at.tid, at.nt);
@@ -91,7 +91,7 @@ __global__ void fp_export_kernel(uint8_t* tiles, const float* outer, int K, int 
                 e2m1_values(h ? c.y : c.x, v);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    r.w[4 * h + i] = FORMAT == MOQE_FP_MXFP4 ? pack_bf16x2(v[2 * i] * s, v[2 * i + 1] * s) : pack_bf16x2(v[2 * i] * s * o, v[2 * i + 1] * s * o);
+                    r.w[4 * h + i] = FORMAT == MOQE_FP_MXFP4 ? bf16_pair(v[2 * i] * s, v[2 * i + 1] * s) : bf16_pair(v[2 * i] * s * o, v[2 * i + 1] * s * o);
             }
         }
         if (values) store32(values + (size_t)n * K + k, (K - k) * 2, wide, r);

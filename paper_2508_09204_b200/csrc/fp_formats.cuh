@@ -106,7 +106,7 @@ __device__ __forceinline__ void e2m1_values(uint32_t codes, float (&v)[8]) {
         v[2 * i] = f.x; v[2 * i + 1] = f.y;
     }
 }
-__device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&h);
 }

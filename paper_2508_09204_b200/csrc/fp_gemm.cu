@@ -331,10 +331,6 @@ __device__ __forceinline__ void tmem_ld_16x256(uint32_t taddr, uint32_t* v) {
           "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
         : "r"(taddr) : "memory");
 }
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&h);
-}
 // Scaled (by channel, w, and token, x of token `lane`) and rounded: o[4 j + b] = tokens 8 j + 2 (lane % 4) + {0, 1} of channel 8 b + lane / 4.
 __device__ __forceinline__ void pack_block(const uint32_t* v, bool scaled, const float (&w)[4], float x, int lane, uint32_t* o) {
 #pragma unroll
@@ -345,7 +341,7 @@ __device__ __forceinline__ void pack_block(const uint32_t* v, bool scaled, const
         for (int b = 0; b < 4; ++b) {
             float lo = __uint_as_float(v[16 * (b >> 1) + 4 * j + 2 * (b & 1)]), hi = __uint_as_float(v[16 * (b >> 1) + 4 * j + 2 * (b & 1) + 1]);
             if (scaled) { lo = lo * w[b] * x0; hi = hi * w[b] * x1; }
-            o[4 * j + b] = pack_bf16(lo, hi);
+            o[4 * j + b] = bf16_pair(lo, hi);
         }
     }
 }

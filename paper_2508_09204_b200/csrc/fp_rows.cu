@@ -33,7 +33,7 @@ __global__ void __maxnreg__(64) fp4_rows_kernel(const __nv_bfloat16* __restrict_
                 e2m1_values(c[h], v);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    r.w[4 * h + i] = FORMAT == MOQE_FP_MXFP4 ? pack_bf16x2(v[2 * i] * s, v[2 * i + 1] * s) : pack_bf16x2(v[2 * i] * s * o, v[2 * i + 1] * s * o);
+                    r.w[4 * h + i] = FORMAT == MOQE_FP_MXFP4 ? bf16_pair(v[2 * i] * s, v[2 * i + 1] * s) : bf16_pair(v[2 * i] * s * o, v[2 * i + 1] * s * o);
             }
             store32(values + m * K + k, (K - k) * 2, wide, r);
         }
@@ -136,11 +136,6 @@ __global__ void fp_tokens_kernel(const __grid_constant__ TokenParams p) {
     }
 }
 
-// Many rows: as many blocks as there is room for, each with a ring of rows that bulk copies bring to shared memory, a place after
-// another.  A block that takes its row from global memory has its loads under way in the L1 cache, of which next to nothing is left
-// on an SM set up for the product's shared memory, and this kernel's first blocks run beside the last of a product (4160 rows of 18944 k in
-// NVFP4 with a product behind them 104 -> 86 us; alone 64 -> 53).  What is left is instructions: two thirds of the issue slots, 250 for 32 x 16
-// numbers, of which a row's own cost 50.  16384 rows of 4096 k: MXFP4 36 us, NVFP4 47, for 26 of HBM.
 // 16 numbers of a row in shared memory, zeros behind its end
 __device__ __forceinline__ void read16(const unsigned char* row, int k, int K, RawBf16& raw) {
     const uint4 z = make_uint4(0, 0, 0, 0), *q = reinterpret_cast<const uint4*>(row + k * 2);
@@ -148,6 +143,7 @@ __device__ __forceinline__ void read16(const unsigned char* row, int k, int K, R
     raw.r.w[0] = a.x; raw.r.w[1] = a.y; raw.r.w[2] = a.z; raw.r.w[3] = a.w;
     raw.r.w[4] = b.x; raw.r.w[5] = b.y; raw.r.w[6] = b.z; raw.r.w[7] = b.w;
 }
+// A token row in shared memory into its place, by the whole block.
 template <int FORMAT>
 __device__ __forceinline__ void pack_ring_row(const unsigned char* row, int K, const PackedRow& out, float* outer, uint32_t* buf) {
     const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 31, padded = fp_kblocks(K, FORMAT) * fp_kbk(FORMAT);
@@ -162,7 +158,10 @@ __device__ __forceinline__ void pack_ring_row(const unsigned char* row, int K, c
         if (m >= 0x7F800000u) {                                // (infinities and NaN do not count)
             m = 0;
             for (int k = tid * 8; k < K; k += nt * 8)
-                for (int i = 0; i < 8; ++i) { const uint32_t b = (uint32_t)(*reinterpret_cast<const uint16_t*>(row + (k + i) * 2) & 0x7FFFu) << 16; m = max(m, b < 0x7F800000u ? b : 0u); }
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t b = (uint32_t)(*reinterpret_cast<const uint16_t*>(row + (k + i) * 2) & 0x7FFFu) << 16;
+                    m = max(m, b < 0x7F800000u ? b : 0u);
+                }
         }
         field = nv_row_field(block_max(m, buf));
         if (tid == 0) *outer = pow2_field(field);
@@ -188,6 +187,11 @@ __device__ __forceinline__ void pack_ring_row(const unsigned char* row, int K, c
         }
     }
 }
+// Many rows: as many blocks as there is room for, each with a ring of rows that bulk copies bring to shared memory, a place after
+// another.  A block that takes its row from global memory has its loads under way in the L1 cache, of which next to nothing is left
+// on an SM set up for the product's shared memory, and this kernel's first blocks run beside the last of a product (4160 rows of 18944 k in
+// NVFP4 with a product behind them 104 -> 86 us; alone 64 -> 53).  What is left is instructions: two thirds of the issue slots, 250 for 32 x 16
+// numbers, of which a row's own cost 50.  16384 rows of 4096 k: MXFP4 36 us, NVFP4 47, for 26 of HBM.
 constexpr int RING_MAX_STAGES = 4, RING_MAX_K = 32768;     // (two rows of 64 KB)
 __global__ void __maxnreg__(64) fp_tokens_ring_kernel(const __grid_constant__ TokenParams p, int stages, int stride, int* status) {
     extern __shared__ __align__(128) unsigned char ring[];
