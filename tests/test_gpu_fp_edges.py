@@ -220,3 +220,49 @@ def test_many_rows_with_infinities_and_rows_of_nobody(M, K):
     hit = bad[(ids[bad] >= 0) & (ids[bad] < 4)]
     four = hit[ids[hit] != 2]
     assert bool(Z[four].isnan().all()) and not bool(Z[hit].isfinite().any())
+
+
+def test_many_rows_captured_with_inputs_that_change():
+    """The rows' ring, the schedule and a sort in one graph, replayed with other rows and another routing; X from a 16-byte boundary only."""
+    M, N, K = 2304, 264, 4104
+    g = np.random.default_rng(21)
+    ex = [_expert(e, N, K, f) for e, f in enumerate([NV, BF, MX])]
+    handles = [e for e, _ in ex]
+    X = torch.zeros(M * K + 8, dtype=torch.bfloat16, device="cuda")[8:].view(M, K)
+    ids = torch.zeros(M, dtype=torch.int32, device="cuda")
+    Y = torch.empty((M, N), dtype=torch.bfloat16, device="cuda")
+    ws = moqe.alloc_workspace(moqe.moqe_routed_fpgemm_workspace(M, handles))
+    moqe.moqe_routed_fpgemm(X, ids, handles, Y=Y, workspace=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        moqe.moqe_routed_fpgemm(X, ids, handles, Y=Y, workspace=ws)
+    for _ in range(4):
+        X.copy_(_bf16(g.standard_normal((M, K))))
+        ids.copy_(_dev(g.integers(0, 3, M).astype(np.int32)))
+        Y.fill_(float("nan"))
+        graph.replay()
+        _check(Y, X, ids, [w for _, w in ex], [NV, BF, MX])
+    assert moqe.moqe_async_status() == moqe.OK
+
+
+@pytest.mark.parametrize("M", [130, 2500])
+def test_an_expert_built_just_before_a_larger_product(M):
+    N, K = 1032, 4096
+    g = np.random.default_rng(M)
+    X = _bf16(g.standard_normal((M, K)))
+    ids = torch.zeros(M, dtype=torch.int32, device="cuda")
+    formats = (MX, NV, BF, NV)
+    W = [_dev((g.standard_normal((N, K)) * 0.02).astype(np.float32)) for _ in formats]
+    ws = moqe.alloc_workspace(moqe.moqe_routed_fpgemm_workspace(M, [moqe.moqe_fp_quantize(W[0], BF)]) + moqe.moqe_routed_fpgemm_workspace(M, [moqe.moqe_fp_quantize(W[1], NV)]))
+    want = [moqe.moqe_routed_fpgemm(X, ids, [moqe.moqe_fp_quantize(w, f)]) for w, f in zip(W, formats)]
+    torch.cuda.synchronize()
+    for _ in range(6):
+        keep = [moqe.moqe_fp_quantize(W[0], MX)]
+        got = []
+        for w, f in zip(W, formats):
+            keep.append(moqe.moqe_fp_quantize(w, f))
+            got.append(moqe.moqe_routed_fpgemm(X, ids, [keep[-1]], workspace=ws))
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+    assert moqe.moqe_async_status() == moqe.OK
