@@ -656,6 +656,7 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
                 uint32_t old = 0;
                 if (lane == 0) old = count_in(p.counters + (w0 * CG + rank) * FP_EPI_WARPS + warp);
                 old = __shfl_sync(0xFFFFFFFFu, old, 0);
+                __syncwarp();                                // (the lane that has acquired them, then the lanes that read: a shuffle orders no memory)
                 // the adding up waits until this worker's other pieces are parked: somebody may be waiting for those
                 if ((int)old == w1 - w0) {
                     if (owed == 0) { owed_at[0] = pc.at; owed_tile[0] = pc.tile; owed_w[0] = w0 | w1 << 16; }
