@@ -140,8 +140,20 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
-def _handles(experts) -> array:
-    """The experts' handles as a C array; pass ``.buffer_info()[0]`` and keep the array until the call returns."""
+def _handle(e, kind):
+    """The handle of ``e``, which has to be a ``kind``: the library cannot tell one kind of handle from another."""
+    if not isinstance(e, kind):
+        raise ValueError(f"{kind.__name__} expected, not {type(e).__name__}")
+    return e.handle
+
+
+def _handles(experts, kind=None) -> array:
+    """The experts' handles as a C array; pass ``.buffer_info()[0]`` and keep the array until the call returns.  ``kind``: what they
+    have to be (an ``Expert``)."""
+    kind = Expert if kind is None else kind
+    for e in experts:
+        if not isinstance(e, kind):
+            raise ValueError(f"{kind.__name__} expected, not {type(e).__name__}")
     return array("Q", [e.address for e in experts])
 
 
@@ -209,7 +221,7 @@ class HostExpert:
 
 def moqe_expert_offload(e: Expert) -> HostExpert:
     out = C.c_void_p()
-    _check(lib().moqe_expert_offload(e.handle, _stream(), C.byref(out)), "moqe_expert_offload")
+    _check(lib().moqe_expert_offload(_handle(e, Expert), _stream(), C.byref(out)), "moqe_expert_offload")
     return HostExpert(out.value)
 
 
@@ -217,12 +229,12 @@ def moqe_expert_prefetch(h: HostExpert, stream: Optional[torch.cuda.Stream] = No
     """Enqueues the host-to-device copies on ``stream`` (default: the current one) and returns the new expert."""
     out = C.c_void_p()
     st = C.c_void_p(stream.cuda_stream) if stream is not None else _stream()
-    _check(lib().moqe_expert_prefetch(h.handle, st, C.byref(out)), "moqe_expert_prefetch")
+    _check(lib().moqe_expert_prefetch(_handle(h, HostExpert), st, C.byref(out)), "moqe_expert_prefetch")
     return Expert(out.value)
 
 
 def moqe_expert_host_save(h: HostExpert, path: str) -> None:
-    _check(lib().moqe_expert_host_save(h.handle, os.fsencode(path)), "moqe_expert_host_save")
+    _check(lib().moqe_expert_host_save(_handle(h, HostExpert), os.fsencode(path)), "moqe_expert_host_save")
 
 
 def moqe_expert_host_load(path: str) -> HostExpert:
@@ -243,11 +255,12 @@ def moqe_quantize_rtn(W: torch.Tensor, bits: int, group: int, sym: bool) -> Expe
 
 def moqe_expert_export(e: Expert) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """-> (codes uint8 [N][K], scales fp16 [N][K/g], zeros fp16 [N][K/g])."""
+    handle = _handle(e, Expert)
     dev = torch.device("cuda", torch.cuda.current_device())
     codes = torch.empty((e.N, e.K), dtype=torch.uint8, device=dev)
     scales = torch.empty((e.N, e.groups_per_row), dtype=torch.float16, device=dev)
     zeros = torch.empty((e.N, e.groups_per_row), dtype=torch.float16, device=dev)
-    _check(lib().moqe_expert_export(e.handle, _ptr(codes), _ptr(scales), _ptr(zeros), _stream()), "moqe_expert_export")
+    _check(lib().moqe_expert_export(handle, _ptr(codes), _ptr(scales), _ptr(zeros), _stream()), "moqe_expert_export")
     return codes, scales, zeros
 
 
@@ -447,7 +460,7 @@ def moqe_routed_qgemm_sorted_multi(Xs: Sequence[torch.Tensor], perm: torch.Tenso
     if _arrs is None:
         xa = array("Q", [_ptr(x) or 0 for x in Xs])
         ya = array("Q", [_ptr(y) or 0 for y in Ys])
-        ea = array("Q", [e.address for layer in experts for e in layer])
+        ea = _handles([e for layer in experts for e in layer])
     else:
         xa, ya, ea = _arrs
     _check(lib().moqe_routed_qgemm_sorted_multi(_at(xa), _ptr(perm), _ptr(offsets), M, nl, _at(ea), E, _at(ya), _ptr(workspace),
@@ -544,18 +557,19 @@ def moqe_fp_expert_import(fmt: int, codes: Optional[torch.Tensor] = None, scales
 
 def moqe_fp_expert_export(e: FpExpert, values: bool = False):
     """-> (codes, scales, outer, values) as ``moqe_fp4_quantize_rows`` gives them; only values for an ``FP_BF16`` expert."""
+    handle = _handle(e, FpExpert)
     dev = torch._C._cuda_getDevice()
     four = e.format != FP_BF16
     codes = _rows_of(e.N, e.K // 2, torch.uint8, dev) if four else None
     scales = _rows_of(e.N, _fp_blocks(e.K, e.format), torch.uint8, dev) if four else None
     outer = torch.empty_strided((e.N,), (1,), dtype=torch.float32, device=dev) if e.format == FP_NVFP4 else None
     vals = _rows_of(e.N, e.K, torch.bfloat16, dev) if values or not four else None
-    _check(lib().moqe_fp_expert_export(e.handle, _ptr(codes), _ptr(scales), _ptr(outer), _ptr(vals), _stream()), "moqe_fp_expert_export")
+    _check(lib().moqe_fp_expert_export(handle, _ptr(codes), _ptr(scales), _ptr(outer), _ptr(vals), _stream()), "moqe_fp_expert_export")
     return codes, scales, outer, vals
 
 
 def moqe_routed_fpgemm_workspace(M: int, experts: Sequence[FpExpert]) -> int:
-    arr = _handles(experts)
+    arr = _handles(experts, FpExpert)
     return int(lib().moqe_routed_fpgemm_workspace(int(M), arr.buffer_info()[0], len(experts)))
 
 
@@ -571,7 +585,7 @@ def moqe_routed_fpgemm(X: torch.Tensor, row_ids: torch.Tensor, experts: Sequence
         Y = torch.empty((M, experts[0].N), dtype=torch.bfloat16, device=X.device)
     if workspace is None:
         workspace = alloc_workspace(moqe_routed_fpgemm_workspace(M, experts), X.device)
-    arr = _handles(experts)
+    arr = _handles(experts, FpExpert)
     _check(lib().moqe_routed_fpgemm(_ptr(X), _ptr(row_ids), M, arr.buffer_info()[0], E, _ptr(Y), _ptr(workspace), workspace.numel(),
                                     _stream()), "moqe_routed_fpgemm")
     return Y
@@ -580,7 +594,7 @@ def moqe_routed_fpgemm(X: torch.Tensor, row_ids: torch.Tensor, experts: Sequence
 def moqe_routed_fpgemm_sorted(X: torch.Tensor, perm: torch.Tensor, offsets: torch.Tensor, experts: Sequence[FpExpert],
                               Y: torch.Tensor, workspace: torch.Tensor, _arr=None) -> torch.Tensor:
     """The same for a batch that ``moqe_permute`` has sorted; rows before ``offsets[0]`` and behind ``offsets[E]`` keep their ``Y``."""
-    arr = _arr if _arr is not None else _handles(experts)
+    arr = _arr if _arr is not None else _handles(experts, FpExpert)
     _check(lib().moqe_routed_fpgemm_sorted(_ptr(X), _ptr(perm), _ptr(offsets), X.shape[0], _at(arr), len(experts), _ptr(Y),
                                            _ptr(workspace), workspace.numel(), _stream()), "moqe_routed_fpgemm_sorted")
     return Y
