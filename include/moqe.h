@@ -54,7 +54,7 @@ typedef enum {
                                   K % 8 != 0; E > MOQE_MAX_EXPERTS; misaligned pointer */
     MOQE_ERR_ALLOC = 4,        /* device allocation failed */
     MOQE_ERR_WORKSPACE = 5,    /* workspace NULL or smaller than the *_workspace() figure */
-    MOQE_ERR_MISMATCH = 6,     /* experts of one call disagree on N or K */
+    MOQE_ERR_MISMATCH = 6,     /* experts of one call disagree on N or K; a floating-point expert is not on the current device */
     MOQE_ERR_CUDA = 7,         /* a CUDA runtime / driver call failed */
     MOQE_ERR_EXPERT_ID = 8,    /* asynchronous: an id outside [0,E) was seen by a kernel */
     MOQE_ERR_TIMEOUT = 9,      /* asynchronous: a bounded in-kernel wait ran out */

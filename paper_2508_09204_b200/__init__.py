@@ -151,10 +151,11 @@ def _handles(experts, kind=None) -> array:
     """The experts' handles as a C array; pass ``.buffer_info()[0]`` and keep the array until the call returns.  ``kind``: what they
     have to be (an ``Expert``)."""
     kind = Expert if kind is None else kind
+    arr = array("Q")
     for e in experts:
-        if not isinstance(e, kind):
-            raise ValueError(f"{kind.__name__} expected, not {type(e).__name__}")
-    return array("Q", [e.address for e in experts])
+        h = _handle(e, kind)
+        arr.append(0 if h is None else h.value or 0)
+    return arr
 
 
 def _dev(t: torch.Tensor, dtype, name: str) -> torch.Tensor:
@@ -162,6 +163,14 @@ def _dev(t: torch.Tensor, dtype, name: str) -> torch.Tensor:
         raise ValueError(f"{name} must be a CUDA tensor")
     if t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}")
+    return t if t.is_contiguous() else t.contiguous()
+
+
+def _here(t: torch.Tensor, dtype, name: str) -> torch.Tensor:
+    """The same for a tensor that has to be on the current device: the call goes to that device's stream."""
+    if t.get_device() != torch._C._cuda_getDevice() or t.dtype != dtype:
+        _dev(t, dtype, name)
+        raise ValueError(f"{name} must be on the current device")
     return t if t.is_contiguous() else t.contiguous()
 
 
@@ -512,7 +521,7 @@ def _rows_of(n: int, m: int, dtype, dev) -> torch.Tensor:
 def moqe_fp4_quantize_rows(X: torch.Tensor, fmt: int, values: bool = False):
     """Rows of bf16 ``X[M][K]`` in a 4-bit format: (codes uint8 ``[M][K/2]``, scales uint8 ``[M][blocks]``, outer fp32 ``[M]`` or
     None, values bf16 ``[M][K]`` or None)."""
-    X = _dev(X, torch.bfloat16, "X")
+    X = _here(X, torch.bfloat16, "X")
     M, K = X.shape
     dev = X.device
     codes = _rows_of(M, K // 2, torch.uint8, dev)
@@ -526,7 +535,7 @@ def moqe_fp4_quantize_rows(X: torch.Tensor, fmt: int, values: bool = False):
 
 def moqe_fp_quantize(W: torch.Tensor, fmt: int) -> FpExpert:
     """The fp32 device matrix ``W[N][K]`` as an expert in ``FP_MXFP4``, ``FP_NVFP4`` or ``FP_BF16``."""
-    W = _dev(W, torch.float32, "W")
+    W = _here(W, torch.float32, "W")
     N, K = W.shape
     out = C.c_void_p()
     _check(lib().moqe_fp_quantize(_ptr(W), N, K, int(fmt), _stream(), C.byref(out)), "moqe_fp_quantize")
@@ -539,13 +548,13 @@ def moqe_fp_expert_import(fmt: int, codes: Optional[torch.Tensor] = None, scales
     if fmt == FP_BF16:
         if values is None:
             raise MoqeError(ERR_NULL, "moqe_fp_expert_import")
-        values = _dev(values, torch.bfloat16, "values")
+        values = _here(values, torch.bfloat16, "values")
         (N, K), codes, scales, outer = values.shape, None, None, None
     else:
         if codes is None or scales is None:
             raise MoqeError(ERR_NULL, "moqe_fp_expert_import")
-        codes, scales, values = _dev(codes, torch.uint8, "codes"), _dev(scales, torch.uint8, "scales"), None
-        outer = None if outer is None or fmt == FP_MXFP4 else _dev(outer, torch.float32, "outer")
+        codes, scales, values = _here(codes, torch.uint8, "codes"), _here(scales, torch.uint8, "scales"), None
+        outer = None if outer is None or fmt == FP_MXFP4 else _here(outer, torch.float32, "outer")
         N, K = codes.shape[0], 2 * codes.shape[1]
         if tuple(scales.shape) != (N, _fp_blocks(K, fmt)) or (outer is not None and outer.numel() != N):
             raise MoqeError(ERR_SHAPE, "moqe_fp_expert_import")
@@ -573,19 +582,43 @@ def moqe_routed_fpgemm_workspace(M: int, experts: Sequence[FpExpert]) -> int:
     return int(lib().moqe_routed_fpgemm_workspace(int(M), arr.buffer_info()[0], len(experts)))
 
 
+_BF16, _I32 = torch.bfloat16, torch.int32
+
+
+def _fp_product(X, rows, offsets, experts, Y, workspace, where: str):
+    """The product's tensors as the library takes them, or the error that says what is wrong with them.  (What is right is found so in one
+    expression: 2 us less than one tensor after another.)"""
+    here, E = torch._C._cuda_getDevice(), len(experts)
+    if E == 0 or X.ndim != 2 or Y.ndim != 2:
+        raise MoqeError(ERR_SHAPE, where)
+    (M, K), (MY, N), first = X.shape, Y.shape, experts[0]
+    if K != first.K or MY < M or N != first.N or rows.numel() < M or (offsets is not None and offsets.numel() <= E):
+        raise MoqeError(ERR_SHAPE, where)
+    if not (X.get_device() == rows.get_device() == Y.get_device() == workspace.get_device() == here
+            and X.dtype is Y.dtype is _BF16 and rows.dtype is _I32
+            and X.is_contiguous() and rows.is_contiguous() and Y.is_contiguous() and workspace.is_contiguous()
+            and (offsets is None or (offsets.get_device() == here and offsets.dtype is _I32 and offsets.is_contiguous()))):
+        for t, dtype, name in ((Y, torch.bfloat16, "Y"), (workspace, workspace.dtype, "workspace")):
+            if not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous")
+            _here(t, dtype, name)
+        X, rows = _here(X, torch.bfloat16, "X"), _here(rows, torch.int32, "row_ids" if offsets is None else "perm")
+        offsets = None if offsets is None else _here(offsets, torch.int32, "offsets")
+    return M, X, rows, offsets
+
+
 def moqe_routed_fpgemm(X: torch.Tensor, row_ids: torch.Tensor, experts: Sequence[FpExpert], Y: Optional[torch.Tensor] = None,
                        workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """``Y[m] = xq[m] . W_{row_ids[m]}^T``: the routed product of floating-point experts of any mixture of formats."""
-    X = _dev(X, torch.bfloat16, "X")
-    row_ids = _dev(row_ids, torch.int32, "row_ids")
     M, E = X.shape[0], len(experts)
-    if E == 0 or row_ids.numel() != M or X.shape[1] != experts[0].K:
+    if E == 0 or row_ids.numel() != M:
         raise MoqeError(ERR_SHAPE, "moqe_routed_fpgemm")
+    arr = _handles(experts, FpExpert)
     if Y is None:
         Y = torch.empty((M, experts[0].N), dtype=torch.bfloat16, device=X.device)
     if workspace is None:
-        workspace = alloc_workspace(moqe_routed_fpgemm_workspace(M, experts), X.device)
-    arr = _handles(experts, FpExpert)
+        workspace = alloc_workspace(lib().moqe_routed_fpgemm_workspace(M, arr.buffer_info()[0], E), X.device)
+    M, X, row_ids, _ = _fp_product(X, row_ids, None, experts, Y, workspace, "moqe_routed_fpgemm")
     _check(lib().moqe_routed_fpgemm(_ptr(X), _ptr(row_ids), M, arr.buffer_info()[0], E, _ptr(Y), _ptr(workspace), workspace.numel(),
                                     _stream()), "moqe_routed_fpgemm")
     return Y
@@ -595,8 +628,10 @@ def moqe_routed_fpgemm_sorted(X: torch.Tensor, perm: torch.Tensor, offsets: torc
                               Y: torch.Tensor, workspace: torch.Tensor, _arr=None) -> torch.Tensor:
     """The same for a batch that ``moqe_permute`` has sorted; rows before ``offsets[0]`` and behind ``offsets[E]`` keep their ``Y``."""
     arr = _arr if _arr is not None else _handles(experts, FpExpert)
-    _check(lib().moqe_routed_fpgemm_sorted(_ptr(X), _ptr(perm), _ptr(offsets), X.shape[0], _at(arr), len(experts), _ptr(Y),
-                                           _ptr(workspace), workspace.numel(), _stream()), "moqe_routed_fpgemm_sorted")
+    M, X, perm, offsets = _fp_product(X, perm, offsets, experts, Y, workspace, "moqe_routed_fpgemm_sorted")
+    code = lib().moqe_routed_fpgemm_sorted(X.data_ptr(), perm.data_ptr(), offsets.data_ptr(), M, _at(arr), len(experts), Y.data_ptr(),
+                                           workspace.data_ptr(), workspace.numel(), _stream())
+    _check(code, "moqe_routed_fpgemm_sorted")
     return Y
 
 

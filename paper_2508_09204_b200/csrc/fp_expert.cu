@@ -167,6 +167,8 @@ extern "C" moqe_status moqe_fp_expert_export(const moqe_fp_expert* e, uint8_t* c
     if ((uintptr_t)codes % 4 || (uintptr_t)outer % 4 || (uintptr_t)values_bf16 % 16) return MOQE_ERR_UNSUPPORTED;
     if (e->format == MOQE_FP_BF16 ? codes || scales || outer : e->format == MOQE_FP_MXFP4 && outer) return MOQE_ERR_UNSUPPORTED;
     if (!codes && !scales && !outer && !values_bf16) return MOQE_OK;
+    const moqe_status here = fp_on_current_device(e);
+    if (here != MOQE_OK) return here;
     cudaStream_t st = (cudaStream_t)stream;
     const auto kernel = e->format == MOQE_FP_MXFP4 ? fp_export_kernel<MOQE_FP_MXFP4> : e->format == MOQE_FP_NVFP4 ? fp_export_kernel<MOQE_FP_NVFP4> : fp_export_kernel<MOQE_FP_BF16>;
     const bool wide = e->K % 16 == 0 && (uintptr_t)codes % 8 == 0 && (uintptr_t)values_bf16 % 32 == 0;

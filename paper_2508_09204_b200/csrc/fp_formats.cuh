@@ -336,6 +336,13 @@ __device__ __forceinline__ void put_packed(const PackedLane& out, int chunk, boo
     if ((threadIdx.x & (4 * LANES - 1)) == 0) *reinterpret_cast<uint32_t*>(out.scale + chunk * out.scale_step) = w;
 }
 
+// a call's kernels run on the current device, and read an expert where it was built
+inline moqe_status fp_on_current_device(const moqe_fp_expert* e) {
+    int now = 0;
+    if (cudaGetDevice(&now) != cudaSuccess) { cudaGetLastError(); return MOQE_ERR_CUDA; }
+    return now == e->device ? MOQE_OK : MOQE_ERR_MISMATCH;
+}
+
 // quantize.cu: device memory of experts (a pool of the library's)
 void* expert_malloc(size_t bytes, int device, cudaStream_t st, bool& pooled);
 bool expert_free(void* p, bool pooled, int device);

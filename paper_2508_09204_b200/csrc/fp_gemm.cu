@@ -804,9 +804,11 @@ moqe_status fp_args(const void* X, const void* rows, const void* offsets, int M,
     for (int e = 0; e < E; ++e)
         if (!ex[e]) return MOQE_ERR_NULL;
     for (int e = 1; e < E; ++e)
-        if (ex[e]->N != ex[0]->N || ex[e]->K != ex[0]->K) return MOQE_ERR_MISMATCH;
+        if (ex[e]->N != ex[0]->N || ex[e]->K != ex[0]->K || ex[e]->device != ex[0]->device) return MOQE_ERR_MISMATCH;
     if (M == 0) return MOQE_OK;
     if (!X || !rows || !offsets || !Y) return MOQE_ERR_NULL;
+    const moqe_status here = fp_on_current_device(ex[0]);
+    if (here != MOQE_OK) return here;
     if (ex[0]->N % 8 != 0 || (uintptr_t)X % 16 || (uintptr_t)Y % 16 || !fp_schedulable(M, ex, E)) return MOQE_ERR_UNSUPPORTED;
     w = fp_layout(M, ex, E);
     if (!workspace || workspace_bytes < w.total || (uintptr_t)workspace % 256) return MOQE_ERR_WORKSPACE;
