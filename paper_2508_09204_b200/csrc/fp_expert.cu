@@ -68,6 +68,12 @@ __global__ void fp_export_kernel(uint8_t* tiles, const float* outer, int K, int 
         o = outer[n];
         if (outer_out && threadIdx.x == 0) outer_out[n] = o;
     }
+    // (a row scale that is a power of two, as of rows quantized here: every product is exact)
+    const bool plain = (__float_as_uint(o) & 0x7FFFFFu) == 0;
+    const auto scaled = [&](float a, float b) {
+        if constexpr (FORMAT != MOQE_FP_NVFP4) return bf16_pair(a, b);
+        return plain ? bf16_pair(a * o, b * o) : bf16_pair(mul_to_odd(a, o), mul_to_odd(b, o));
+    };
     const int blocks = (K + fp_block(FORMAT) - 1) / fp_block(FORMAT);
     for (int k = threadIdx.x * 16; k < K; k += blockDim.x * 16) {
         Raw32 r;
@@ -91,7 +97,7 @@ __global__ void fp_export_kernel(uint8_t* tiles, const float* outer, int K, int 
                 e2m1_values(h ? c.y : c.x, v);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    r.w[4 * h + i] = FORMAT == MOQE_FP_MXFP4 ? bf16_pair(v[2 * i] * s, v[2 * i + 1] * s) : bf16_pair(v[2 * i] * s * o, v[2 * i + 1] * s * o);
+                    r.w[4 * h + i] = scaled(v[2 * i] * s, v[2 * i + 1] * s);
             }
         }
         if (values) store32(values + (size_t)n * K + k, (K - k) * 2, wide, r);

@@ -106,6 +106,12 @@ __device__ __forceinline__ void e2m1_values(uint32_t codes, float (&v)[8]) {
         v[2 * i] = f.x; v[2 * i + 1] = f.y;
     }
 }
+// a * b to odd: of the two fp32 numbers around a product that fp32 does not hold, the one whose last bit is set.  Rounded to bf16 after
+// that it is the product rounded once (an fp32 nearest to it can be half way between two bf16 numbers where the product is not).
+__device__ __forceinline__ float mul_to_odd(float a, float b) {
+    const float below = __fmul_rd(a, b), above = __fmul_ru(a, b);
+    return __float_as_uint(below) & 1u ? below : above;
+}
 __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&h);
