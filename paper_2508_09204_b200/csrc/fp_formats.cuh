@@ -316,7 +316,7 @@ constexpr int ROWS_OF_WARPS = 4;
 struct RowLaunch { int blocks, threads; };
 inline RowLaunch row_launch(int rows, int K, int chunks) {
     const int t = row_threads(K, chunks);
-    return t > 32 ? RowLaunch{rows, t} : RowLaunch{(rows + ROWS_OF_WARPS - 1) / ROWS_OF_WARPS, 32 * ROWS_OF_WARPS};
+    return t > 32 ? RowLaunch{rows, t} : RowLaunch{rows / ROWS_OF_WARPS + (rows % ROWS_OF_WARPS != 0), 32 * ROWS_OF_WARPS};   // (any int of rows)
 }
 // which row this thread works on, as which of how many threads
 struct RowPlace { int row, tid, nt; };
