@@ -6,8 +6,9 @@
 // Every rounding here is that of an exact real quotient.  MXFP4 divides by a power of two.  NVFP4 divides by an e4m3 number.  For a
 // source of bf16 a quotient that is not half way between two numbers is at least 2^-9 of its size away from there: a product with a
 // reciprocal that is a little too large, cut to 12 bits, is the half way mark where the quotient is, and on the quotient's side of it
-// elsewhere.  For fp32 it is 2^-24 of its size away, so that the correctly rounded fp32 quotient can meet a half way mark that it should
-// not meet, and there the sign of the remainder decides (nv_quotient).
+// elsewhere.  For fp32 the nearest quotient beside a mark is more than half a unit of the mark's last place away from it, so that a
+// correctly rounded one would never meet a mark wrongly; the one worked out here is a unit off at most, but not shown to be correctly
+// rounded, so that on a mark the sign of the remainder decides (nv_quotient).
 //
 // Packed layout, the same for experts and for a call's token rows: k-blocks of 128 bytes a row (256 codes or 64 bf16), in which a
 // row's eight 16-byte chunks are permuted by the 128-byte swizzle (chunk c of row r at place c ^ (r & 7)), eight rows to 1024
@@ -123,9 +124,9 @@ __device__ __forceinline__ uint32_t e4m3_byte(float v) {
     return d & 0xFFu;
 }
 
-// y / s, rounded to nearest, for s > 0 with 1 / s to an unit or two of the last place in rs (one step of Markstein's correction: where
-// the quotient has few bits, as on a border, it is exact).  fp32 sources: moved off a border by a unit of the last place where it
-// is not there exactly, as the remainder's sign says.
+// y / s for s > 0, one of the two fp32 numbers around it, and itself where that is one; 1 / s to an unit or two of the last place in rs
+// (one step of Markstein's correction).  fp32 sources: moved off a border by a unit of the last place where it is not there exactly,
+// as the remainder's sign says.
 template <bool FP32>
 __device__ __forceinline__ float nv_quotient(float y, float s, float rs) {
     const float q0 = y * rs;
