@@ -381,8 +381,9 @@ MOQE_API moqe_status moqe_fp_expert_destroy(moqe_fp_expert* e);
 
 /* The routed product, grouped by expert with ragged sizes, from one row to whole prompts:
  *   Y[m][n] = bf16( sum_k xq[m][k] * w_e[n][k] ),   e = row_ids[m]
- * with fp32 sums (of code * scale; an outer scale of the channel, then the row's, is applied to the sum).  xq = the row quantized to the format of ITS expert (the values of moqe_fp4_quantize_rows) where that is a 4-bit
- * format -- both operands have 4 bits and go to the tensor cores with their scales -- and the row itself where it is BF16.
+ * with fp32 sums (of code * scale; an outer scale of the channel, then the row's, is applied to the sum).  xq = the row quantized
+ * to the format of ITS expert (the values of moqe_fp4_quantize_rows) where that is a 4-bit format -- both operands have 4 bits and go
+ * to the tensor cores with their scales -- and the row itself where it is BF16.
  * The experts of a call may have any mixture of formats; they agree on N (a multiple of 8) and K.  The same call gives the
  * same bits.  workspace: moqe_routed_fpgemm_workspace(M, h_experts, E) bytes (0 for refused arguments), 256-byte aligned, contents
  * irrelevant; the figure grows with M; calls that share a workspace must not overlap on the device.

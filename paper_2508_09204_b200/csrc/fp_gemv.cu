@@ -3,10 +3,14 @@
 //
 //   Y[perm[j]][n] = bf16( o_x o_w[n] sum_b sx[b] sw[n][b] sum_{k in b} cx[k] cw[n][k] )
 //
-// Bound by HBM: 4.25 or 4.5 bits a weight.  The tensor-core kernel needs the row quantized by a kernel before it, splits few tiles along k
-// and adds parked sums up, which is most of its time here (4096 channels x 11008 k: 12.6 us, of which 3.7 are the bytes'; this
-// kernel 8.6).  So a block of 4 to 16 warps takes 32 channels and all of k: nothing is added up outside the block, and every block
-// quantizes the row for itself while its first weights are on their way.
+// 4.25 or 4.5 bits a weight have to come from HBM, but latency counts as much: the row's place, its numbers and their quantization come
+// one after the other before the first weight is multiplied.  The tensor-core kernel needs the row quantized by a kernel before
+// it, splits few tiles along k and adds parked sums up, which is most of its time here.  So a block of 4 to 16 warps takes 32
+// channels and all of k: nothing is added up outside the block, and every block quantizes the row for itself while its first
+// weights are on their way.  A row in a chain of calls, experts in turn so that weights come from HBM, us (the bytes' time; the
+// tensor-core kernel): 11008 k -> 4096 MXFP4 9.1 (3.7; 13.7), NVFP4 10.1 (3.9; 14.7), bf16 17.0 (13.9; 23.6); 4096 k -> 4096 5.6 (1.4;
+// 10.3), 6.1 (1.5; 10.5), 8.4 (5.2; 15.3); 4096 k -> 11008 10.6 (3.7; 11.3), 11.5 (3.9; 11.5), 18.7 (13.9; 25.2).  The same expert again and
+// again, its weights in L2: 11008 k -> 4096 8.2, 8.8, 11.4.
 //
 // A 4-bit number doubled is a whole number, {0, 1, 2, 3, 4, 6, 8, 12} and a sign, so that the products of a block of codes are
 // summed exactly in integers, four to an instruction; the two scales and the row scales are applied in fp32.  One byte permutation looks

@@ -7,8 +7,8 @@
 namespace moqe {
 namespace {
 
-// (Held to 64 registers, a few of which NVFP4 with four chunks spills, more rows are under way on an SM: 16384 x 11008 NVFP4 116 -> 95 us, with
-// values 154 -> 135, MXFP4 74.6 -> 70.8 and 120.8 -> 122.9.)
+// (Held to 64 registers, of which both formats spill a few with four chunks (24 and 56 bytes stored), more rows are under way on an SM: 16384 x
+// 11008 NVFP4 116 -> 95 us, with values 154 -> 135, MXFP4 74.6 -> 70.8 and 120.8 -> 122.9.)
 template <int FORMAT, int CHUNKS>
 __global__ void __maxnreg__(64) fp4_rows_kernel(const __nv_bfloat16* __restrict__ X, int M, int K, bool wide, bool warps, uint8_t* codes, uint8_t* scales, float* outer, __nv_bfloat16* values) {
     __shared__ uint32_t buf[32];
@@ -97,8 +97,11 @@ struct TokenSegments {
 };
 
 // Few rows, or very long ones: a block, or one warp of it, a place j.  (The other kernel, which comes to its first row later but to the
-// next ones sooner, takes over at 9 million numbers; both with the product behind them, us: 2048 x 1024 9.9 and 10.8, 2048 x 4096 18.9 and
-// 19.2, 512 x 18944 37.7 and 30.0, 16384 x 512 22.8 and 21.3.)
+// next ones sooner, takes over at 9 million numbers.  Both with a product of 1024 channels in MXFP4 behind them, rows not in L2, this
+// kernel / the other, us: 1953 rows of 512 k 10.1 / 10.5, 976 x 1024 8.8 / 9.4, 488 x 4096 11.7 / 12.0; 18554 x 512 31.0 / 28.0, 4638 x 2048
+// 21.5 / 20.6, 2319 x 4096 21.2 / 19.5, 501 x 18944 30.1 / 25.1.  They really cross at 4 to 6 million, for the longest rows at 2, so that
+// between there and 9 million this kernel is the slower one: 16384 x 512 29.3 / 26.2, 1025 x 8192 23.5 / 22.1, 443 x 18944 27.7 / 23.7 (NVFP4
+// 31.8 / 25.4), 105 x 18944 19.6 / 17.8.)
 __global__ void fp_tokens_kernel(const __grid_constant__ TokenParams p) {
     __shared__ uint32_t buf[32];
     // the product behind this kernel may read the offset table before this kernel has ended, so nothing is let go before the wait
@@ -255,6 +258,9 @@ __global__ void __maxnreg__(64) fp_tokens_ring_kernel(const __grid_constant__ To
     }
 }
 
+// Four chunks to a thread from 1024 rows on.  Two / four, with values, rows not in L2, us.  NVFP4: 16384 x 11008 175 / 130, 4096 x 18944
+// 86 / 62, 1024 x 11008 12.6 / 11.4; 16 x 4096 2.3 / 3.2, 512 x 4096 3.9 / 4.7.  What short rows pay: 1024 x 4096 5.2 / 6.5, 2048 x 4096 8.2 / 8.8, 16384
+// x 512 9.2 / 11.0.  MXFP4 gains from 18944 k only (4096 rows 62 / 57; 16384 x 11008 124 / 125) and pays up to 14 % below (1024 x 4096 4.6 / 5.2).
 int row_chunks(int M) { return M < 1024 ? 2 : 4; }
 
 }  // namespace
