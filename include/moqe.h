@@ -386,7 +386,9 @@ MOQE_API moqe_status moqe_fp_expert_destroy(moqe_fp_expert* e);
  * to the tensor cores with their scales -- and the row itself where it is BF16.
  * The experts of a call may have any mixture of formats; they agree on N (a multiple of 8) and K.  The same call gives the
  * same bits.  workspace: moqe_routed_fpgemm_workspace(M, h_experts, E) bytes (0 for refused arguments), 256-byte aligned, contents
- * irrelevant; the figure grows with M; calls that share a workspace must not overlap on the device.
+ * irrelevant; the figure grows with M; calls that share a workspace must not overlap on the device.  What a call leaves in it is not
+ * zero: memory that sorted calls of integer experts take as their workspace too has to be cleared again before these
+ * (moqe_routed_qgemm_workspace_clear), so a batch over both kinds wants two.
  * _sorted: `perm` [M] and `offsets` [E+1] as moqe_permute wrote them, not decreasing, within [0, M].  offsets[0] need not be 0: rows
  * perm[0..offsets[0]) and perm[offsets[E]..M) of Y are left untouched, so that a batch over integer and floating-point
  * experts takes one sort, moqe_routed_qgemm_sorted with the first offsets and this call with the rest.

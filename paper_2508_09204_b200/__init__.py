@@ -626,7 +626,10 @@ def moqe_routed_fpgemm(X: torch.Tensor, row_ids: torch.Tensor, experts: Sequence
 
 def moqe_routed_fpgemm_sorted(X: torch.Tensor, perm: torch.Tensor, offsets: torch.Tensor, experts: Sequence[FpExpert],
                               Y: torch.Tensor, workspace: torch.Tensor, _arr=None) -> torch.Tensor:
-    """The same for a batch that ``moqe_permute`` has sorted; rows before ``offsets[0]`` and behind ``offsets[E]`` keep their ``Y``."""
+    """The same for a batch that ``moqe_permute`` has sorted; rows before ``offsets[0]`` and behind ``offsets[E]`` keep their ``Y``.
+
+    ``workspace`` is not one that sorted calls of integer experts use: theirs has to stay clear.
+    """
     arr = _arr if _arr is not None else _handles(experts, FpExpert)
     M, X, perm, offsets = _fp_product(X, perm, offsets, experts, Y, workspace, "moqe_routed_fpgemm_sorted")
     code = lib().moqe_routed_fpgemm_sorted(X.data_ptr(), perm.data_ptr(), offsets.data_ptr(), M, _at(arr), len(experts), Y.data_ptr(),
