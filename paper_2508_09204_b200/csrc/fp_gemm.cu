@@ -30,7 +30,10 @@
 namespace moqe {
 namespace {
 
-constexpr int FP_COST_4BIT = 5, FP_COST_BF16 = 4;      // of a k-block (16 rows x 4096 -> 11008, equal costs: bf16 tiles were done after 22, 4-bit ones after 27 us)
+// Of a k-block.  (16 rows x 4096 -> 11008, equal costs: bf16 tiles were done after 22, 4-bit ones after 27 us.  Whole calls with 4, 5 and 6 to
+// 4: four experts 38.9, 35.6 and 35.3, three experts 28.8, 29.0 and 29.8; 40 x 11008 -> 4096, three 35.0, 33.0 and 33.6; 777 x 2056 -> 1000, four 19.1,
+// 14.8 and 14.8; 4160 x 18944 -> 3584, two 286, 286 and 300, three 264, 273 and 272; others within 2 %.)
+constexpr int FP_COST_4BIT = 5, FP_COST_BF16 = 4;
 constexpr int FP_BAND = 8;                       // token tiles that are gone through together (see FpWalk)
 constexpr int FP_EPI_WARPS = 8;
 constexpr int FP_WEIGHTS_WARP = FP_EPI_WARPS, FP_MMA_WARP = FP_EPI_WARPS + 1, FP_TOKENS_WARP = FP_EPI_WARPS + 2;
@@ -745,7 +748,9 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp_gemm_kernel(const __grid_con
 // MXFP4 28.2 us, with one SM to a tile 35.1, 600 rows 15.3 and 17.6, 8192 rows bf16 238 and 312; 4096 -> 1024, 2048 rows in NVFP4 and bf16
 // 38.3 with pairs, 34.0 without).  One SM's tiles take 64 tokens instead of 128 where the larger ones would leave SMs without and a call
 // has both kinds of experts, bf16 ones four times as deep (777 rows, 2056 -> 1000, three formats: 16.5 us, with 128 tokens 20.7;
-// 4-bit experts only 12.5 and 11.9, bf16 only 19.8 and 19.4 (512 channels of 3584 k)).
+// 4-bit experts only 12.5 and 11.9, bf16 only 19.8 and 19.4 (512 channels of 3584 k)).  Three formats, rows spread evenly, weights not in L2,
+// 64 / 128: 200 x 2056 -> 1000 14.8 / 16.9, 512 x 3584 -> 512 17.8 / 18.6, 1000 x 3584 -> 512 20.9 / 23.5, 500 x 2048 -> 2048 14.4 / 19.3, 256 x 4096 -> 4096
+// 21.7 / 23.6; the slower choice for many rows of a long k: 1500 x 8200 -> 520 33.7 / 32.4, over two formats and skewed 40.3 / 36.9.
 struct FpTile { int TN; bool pair; };
 FpTile pick_tile(int M, const moqe_fp_expert* const* ex, int E) {
     if (M <= 64) return {M <= 16 ? 16 : M <= 32 ? 32 : 64, false};
